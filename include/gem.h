@@ -400,6 +400,164 @@ int gem_sync(gem_t* g);
  * (hipStream_t or NULL). */
 int gem_copy_f32(const float* src, float* dst, int64_t count, void* stream);
 
+/*
+ * ---- operators of a language model's workers --------------------------------
+ *
+ * What a worker computes from data before it has an update to commit: the
+ * scores of a model's logits (a teacher's record, an evaluation), the
+ * distillation loss against such a record with its gradient, and a gated
+ * linear recurrence with its backward pass.  Unlike the commits, which are
+ * held to fixed bits, their values are those of the formulas up to rounding:
+ * inputs are binary32 or bfloat16 (GEM_F32, GEM_BF16), sums, states and
+ * statistics are binary32, and outputs of the inputs' type are rounded once
+ * (nearest even).  Two calls with the same arguments give the same bits: no
+ * sum depends on the order in which blocks run.
+ *
+ * Calls take a gem_ops_t, which holds a stream and a scratch, and are queued
+ * on that stream without synchronising; they allocate nothing and can be
+ * captured in a HIP graph.  Calls on one gem_ops_t must not overlap.  Data
+ * pointers are device memory, aligned to their element size (GEM_EALIGN
+ * otherwise); a matrix is given by the address of its first element and the
+ * elements between the starts of its rows (0: rows follow each other).
+ * Addresses and strides that are multiples of 16 bytes are fastest.  Outputs
+ * must not overlap inputs or each other, but for the two cases named below.
+ */
+typedef struct gem_ops_handle gem_ops_t;
+
+/* Largest vocabulary, and the most alternatives of a row. */
+#define GEM_VOCAB_MAX (1 << 24)
+#define GEM_TOP_MAX 128
+
+/* Create the handle on the current device.  stream is the hipStream_t its work
+ * is queued on (NULL: the device's null stream) and must outlive it.
+ * scratch_bytes is the largest gem_scan_scratch of the recurrences it is used
+ * for, 0 if none.  Errors: EINVAL, ENOMEM, EHIP. */
+int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out);
+
+/* Free the scratch (after the stream drains) and the handle. */
+int gem_ops_destroy(gem_ops_t* ops);
+
+/* rows (at most 2^22) x vocab logits, element (r, v) at data[r * stride + v],
+ * divided by temperature (finite, > 0) before anything else. */
+typedef struct {
+    const void* data;
+    int64_t rows;
+    int64_t stride;
+    int32_t vocab;
+    int32_t dtype;
+    float temperature;
+    int32_t reserved;
+} gem_logits;
+
+/* Outputs of gem_token_scores; any may be NULL. */
+typedef struct {
+    float* logprob;       /* [rows][n_tokens] log probability of each given token */
+    float* entropy;       /* [rows] entropy of the row's distribution, in nats */
+    float* lse;           /* [rows] log of the sum of exponentials */
+    int32_t* top_ids;     /* [rows][top_k] the likeliest tokens */
+    float* top_logprob;   /* [rows][top_k] and their log probabilities */
+} gem_scores;
+
+/* Scores of rows of logits: with z = logits / temperature, lse = log sum_v
+ * exp z_v, the log probability z_v - lse of each of the n_tokens given tokens
+ * of a row (tokens: [rows][n_tokens], may be NULL if n_tokens is 0), the
+ * entropy, and the top_k (0 <= top_k <= GEM_TOP_MAX) tokens of the largest
+ * logits in falling order, equal logits by rising token.  A given token outside
+ * [0, vocab) (padding) has log probability 0.  Logits of -inf are tokens that
+ * cannot occur: they are no alternatives, and where fewer than top_k are left
+ * the list ends with tokens -1 of log probability -inf.  A row of -inf alone
+ * has lse -inf, entropy 0 and log probabilities -inf.  A row with a NaN or
+ * +inf has NaN for its lse, entropy and log probabilities (as far as they are
+ * not -inf or 0 by the above); its alternatives are those of its other
+ * logits, +inf included.  Errors: EINVAL, EDTYPE, EALIGN. */
+int gem_token_scores(gem_ops_t* ops, const gem_logits* z, const int32_t* tokens,
+                     int32_t n_tokens, int32_t top_k, const gem_scores* out);
+
+/* What a teacher holds likely: for each row k tokens and their log
+ * probabilities (both [rows][k]; 1 <= k <= GEM_TOP_MAX), as gem_token_scores
+ * gives them at the same temperature.  Entries whose token is outside
+ * [0, vocab) are no entries; of several with one token the first counts.
+ * tail 0: the entries are a distribution of their own (their probabilities are
+ * scaled to sum 1).  tail 1: they are part of the teacher's distribution, and
+ * what is missing to 1 stands for all tokens that are not listed, as one more
+ * outcome. */
+typedef struct {
+    const int32_t* ids;
+    const float* logprob;
+    int32_t k;
+    int32_t tail;
+} gem_teacher;
+
+/* Distillation loss of each row: the Kullback-Leibler divergence
+ *     loss = sum_i p_i (log p_i - log q_{id_i})  [+ p_t (log p_t - log q_t)]
+ * of q = softmax(logits / temperature) from the teacher's p; with tail, p_t =
+ * max(0, 1 - sum_i p_i) and q_t = sum of q over unlisted tokens.  Outcomes with
+ * p = 0 add nothing; a row without entries has loss 0.  weight ([rows], NULL:
+ * all 1) is the factor of the row's loss in what is minimised: it does not
+ * multiply loss[r], but a row of weight 0 (padding) has loss 0 and its logits
+ * are not read.  Errors: EINVAL, EDTYPE, EALIGN. */
+int gem_distill_loss(gem_ops_t* ops, const gem_logits* z, const gem_teacher* teacher,
+                     const float* weight, float* loss);
+
+/* The same and its gradient: grad (rows x vocab of the logits' type,
+ * grad_stride elements between rows) receives
+ *     weight[r] / temperature * (q_v - p_v)               for a listed token
+ *     weight[r] / temperature * q_v (1 [- p_t / q_t])     for another,
+ * zero in rows of weight 0.  loss may be NULL.  grad may be the logits' own
+ * memory (same address and stride).  A row of logits that are all -inf has
+ * loss +inf and q = 0 in its gradient.  Errors: EINVAL, EDTYPE, EALIGN. */
+int gem_distill_grad(gem_ops_t* ops, const gem_logits* z, const gem_teacher* teacher,
+                     const float* weight, float* loss, void* grad, int64_t grad_stride);
+
+/* Inputs of the gated linear recurrence over `sequences` (>= 1) sequences of
+ * tokens x channels, packed one after the other:
+ *     a_t = sigmoid(gate_t);  h_t = a_t h_{t-1} + (1 - a_t) x_t
+ * for each channel, from h0 ([sequences][channels] binary32; NULL: zeros).
+ * offsets ([sequences + 1] on the device, rising from 0 to tokens) gives each
+ * sequence's first token; equal neighbours are an empty sequence.  NULL: all
+ * have tokens / sequences tokens.  The offsets are read by the kernels and are
+ * not checked on the host; whatever they hold, no access leaves the arrays.
+ * x and gate are of dtype. */
+typedef struct {
+    const void* x;
+    const void* gate;
+    const int64_t* offsets;
+    const float* h0;
+    int64_t tokens;
+    int64_t x_stride;
+    int64_t gate_stride;
+    int32_t channels;
+    int32_t sequences;
+    int32_t dtype;
+    int32_t reserved;
+} gem_scan;
+
+/* Scratch bytes that a gem_ops_t needs for recurrences of these sizes (the same
+ * for both directions), and the rows of the states that forward keeps for
+ * backward. */
+int gem_scan_scratch(int64_t tokens, int32_t channels, int64_t* bytes);
+int gem_scan_state_rows(int64_t tokens, int64_t* rows);
+
+/* y = h for every token (dtype), and h_last ([sequences][channels] binary32,
+ * may be NULL) after each sequence's last (h0 for an empty one).  h_last may
+ * be h0's own memory, so that a state is kept in place: a call with one token
+ * a sequence is the answering step.  states, if not NULL, receives
+ * gem_scan_state_rows(tokens) rows of channels binary32 values for
+ * gem_scan_backward.  Errors: EINVAL, EDTYPE, EALIGN, ESCRATCH. */
+int gem_scan_forward(gem_ops_t* ops, const gem_scan* s, void* y, int64_t y_stride, float* h_last,
+                     float* states);
+
+/* The backward pass: from dy (dtype) and dh_last (binary32, NULL: zeros), with
+ * the states of the forward call on the same inputs,
+ *     r_t = dy_t + a_{t+1} r_{t+1}   (dh_last in place of a_{t+1} r_{t+1} at a sequence's end)
+ *     dx_t = (1 - a_t) r_t;  dgate_t = a_t (1 - a_t) (h_{t-1} - x_t) r_t;  dh0 = a_0 r_0
+ * (dh0 = dh_last for an empty sequence).  dh0 may be NULL.  h is formed again
+ * in binary32 from the states, so its rounding to dtype does not enter the
+ * gradients.  Errors: EINVAL, EDTYPE, EALIGN, ESCRATCH. */
+int gem_scan_backward(gem_ops_t* ops, const gem_scan* s, const float* states, const void* dy,
+                      int64_t dy_stride, const float* dh_last, void* dx, int64_t dx_stride,
+                      void* dgate, int64_t dgate_stride, float* dh0);
+
 #ifdef __cplusplus
 }
 #endif

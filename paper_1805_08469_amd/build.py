@@ -11,7 +11,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgem.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("gem_kernels.hip", "gem_api.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("gem_kernels.hip", "gem_api.cpp", "gem_logits.hip",
+                                            "gem_scan.hip", "gem_ops.cpp")]
 # Device self-tests of the numerics (used by the test suite only).
 SELFTEST_LIB = os.path.join(HERE, "libgem_selftest.so")
 SELFTEST_SOURCES = [os.path.join(CSRC, "gem_selftest.hip")]

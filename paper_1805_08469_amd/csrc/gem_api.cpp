@@ -13,6 +13,7 @@
 #include "../../include/gem.h"
 #include "gem_device.hpp"
 #include "gem_internal.hpp"
+#include "gem_ops.hpp"
 
 using gemk::PassArgs;
 using gemk::SegArgs;
@@ -70,16 +71,21 @@ struct gem_handle {
     void* scratch = nullptr;         // this device's static scratch (gem_gather_static)
 };
 
+static thread_local char g_last_error[512] = "";
+
+void gemk::note_hip_error(const char* file, const char* what, hipError_t e, int line)
+{
+    std::snprintf(g_last_error, sizeof(g_last_error), "%s failed at %s:%d: %s (%d)", what, file,
+                  line, hipGetErrorString(e), static_cast<int>(e));
+}
+
 namespace {
 
 constexpr int64_t kRowAlign = 64;
 
-thread_local char g_last_error[512] = "";
-
 void note_hip_error(const char* what, hipError_t e, int line)
 {
-    std::snprintf(g_last_error, sizeof(g_last_error), "%s failed at gem_api.cpp:%d: %s (%d)", what,
-                  line, hipGetErrorString(e), static_cast<int>(e));
+    gemk::note_hip_error("gem_api.cpp", what, e, line);
 }
 
 #define GEM_HIP(expr)                                        \

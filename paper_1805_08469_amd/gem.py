@@ -39,6 +39,8 @@ GEM_SNAPSHOT, GEM_MOMENT = 0, 1
 GEM_K_MAX = 32
 GEM_P_MAX = 1 << 31
 GEM_PI_BINS = 643
+GEM_VOCAB_MAX = 1 << 24
+GEM_TOP_MAX = 128
 
 # Every symbol include/gem.h declares.
 EXPORTED = (
@@ -49,6 +51,9 @@ EXPORTED = (
     "gem_stats", "gem_stats_reset", "gem_save", "gem_load", "gem_sync", "gem_copy_f32",
     "gem_pi_hist_start", "gem_pi_hist_start_segments", "gem_pi_hist_read", "gem_set_segments",
     "gem_set_cache_policy", "gem_dims", "gem_gather_static",
+    "gem_ops_create", "gem_ops_destroy", "gem_token_scores", "gem_distill_loss",
+    "gem_distill_grad", "gem_scan_scratch", "gem_scan_state_rows", "gem_scan_forward",
+    "gem_scan_backward",
 )
 
 
@@ -75,6 +80,29 @@ class gem_diag_t(C.Structure):
 
 class gem_stats_t(C.Structure):
     _fields_ = [("commits", C.c_int64), ("passes", C.c_int64), ("alg_bytes", C.c_double)]
+
+
+class gem_logits(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("stride", C.c_int64),
+                ("vocab", C.c_int32), ("dtype", C.c_int32), ("temperature", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class gem_scores(C.Structure):
+    _fields_ = [("logprob", C.c_void_p), ("entropy", C.c_void_p), ("lse", C.c_void_p),
+                ("top_ids", C.c_void_p), ("top_logprob", C.c_void_p)]
+
+
+class gem_teacher(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("logprob", C.c_void_p), ("k", C.c_int32),
+                ("tail", C.c_int32)]
+
+
+class gem_scan(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("gate", C.c_void_p), ("offsets", C.c_void_p),
+                ("h0", C.c_void_p), ("tokens", C.c_int64), ("x_stride", C.c_int64),
+                ("gate_stride", C.c_int64), ("channels", C.c_int32), ("sequences", C.c_int32),
+                ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 class GemError(RuntimeError):
@@ -135,6 +163,18 @@ def _load():
         "gem_pi_hist_start_segments": (C.c_int, [vp, C.c_int64]),
         "gem_set_segments": (C.c_int, [vp, i64p, C.c_int32]),
         "gem_pi_hist_read": (C.c_int, [vp, C.POINTER(C.c_uint32), C.c_int64, i64p]),
+        "gem_ops_create": (C.c_int, [C.c_int64, vp, C.POINTER(vp)]),
+        "gem_ops_destroy": (C.c_int, [vp]),
+        "gem_token_scores": (C.c_int, [vp, C.POINTER(gem_logits), vp, C.c_int32, C.c_int32,
+                                       C.POINTER(gem_scores)]),
+        "gem_distill_loss": (C.c_int, [vp, C.POINTER(gem_logits), C.POINTER(gem_teacher), vp, vp]),
+        "gem_distill_grad": (C.c_int, [vp, C.POINTER(gem_logits), C.POINTER(gem_teacher), vp, vp,
+                                       vp, C.c_int64]),
+        "gem_scan_scratch": (C.c_int, [C.c_int64, C.c_int32, i64p]),
+        "gem_scan_state_rows": (C.c_int, [C.c_int64, i64p]),
+        "gem_scan_forward": (C.c_int, [vp, C.POINTER(gem_scan), vp, C.c_int64, vp, vp]),
+        "gem_scan_backward": (C.c_int, [vp, C.POINTER(gem_scan), vp, vp, C.c_int64, vp, vp,
+                                        C.c_int64, vp, C.c_int64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -385,7 +425,58 @@ def gem_copy_f32(src_dev: int, dst_dev: int, count: int, stream: int | None = No
     return _L.gem_copy_f32(src_dev, dst_dev, count, stream or None)
 
 
-# ---- a small owning wrapper used by the tests and the benchmark ----------------
+# ---- the worker's operators, name for name ---------------------------------------
+# Addresses of device memory, 0 or None for an argument that is left out; strides in
+# elements, 0 for rows that follow each other.
+def gem_ops_create(scratch_bytes: int = 0, stream: int | None = None) -> int:
+    out = C.c_void_p()
+    _check(_L.gem_ops_create(scratch_bytes, stream or None, C.byref(out)), "gem_ops_create")
+    return out.value
+
+
+def gem_ops_destroy(ops: int) -> None:
+    _check(_L.gem_ops_destroy(ops), "gem_ops_destroy")
+
+
+def gem_token_scores(ops: int, z: gem_logits, tokens: int, n_tokens: int, top_k: int,
+                     out: gem_scores) -> None:
+    _check(_L.gem_token_scores(ops, C.byref(z), tokens, n_tokens, top_k, C.byref(out)),
+           "gem_token_scores")
+
+
+def gem_distill_loss(ops: int, z: gem_logits, teacher: gem_teacher, weight: int, loss: int) -> None:
+    _check(_L.gem_distill_loss(ops, C.byref(z), C.byref(teacher), weight, loss), "gem_distill_loss")
+
+
+def gem_distill_grad(ops: int, z: gem_logits, teacher: gem_teacher, weight: int, loss: int,
+                     grad: int, grad_stride: int) -> None:
+    _check(_L.gem_distill_grad(ops, C.byref(z), C.byref(teacher), weight, loss, grad, grad_stride),
+           "gem_distill_grad")
+
+
+def gem_scan_scratch(tokens: int, channels: int) -> int:
+    out = C.c_int64()
+    _check(_L.gem_scan_scratch(tokens, channels, C.byref(out)), "gem_scan_scratch")
+    return out.value
+
+
+def gem_scan_state_rows(tokens: int) -> int:
+    out = C.c_int64()
+    _check(_L.gem_scan_state_rows(tokens, C.byref(out)), "gem_scan_state_rows")
+    return out.value
+
+
+def gem_scan_forward(ops: int, s: gem_scan, y: int, y_stride: int, h_last: int, states: int) -> None:
+    _check(_L.gem_scan_forward(ops, C.byref(s), y, y_stride, h_last, states), "gem_scan_forward")
+
+
+def gem_scan_backward(ops: int, s: gem_scan, states: int, dy: int, dy_stride: int, dh_last: int,
+                      dx: int, dx_stride: int, dgate: int, dgate_stride: int, dh0: int) -> None:
+    _check(_L.gem_scan_backward(ops, C.byref(s), states, dy, dy_stride, dh_last, dx, dx_stride,
+                                dgate, dgate_stride, dh0), "gem_scan_backward")
+
+
+# ---- small owning wrappers used by the tests, the benchmark and the example -------
 class Gem:
     """Owns one libgem handle.  ``stream`` is a hipStream_t address or None."""
 
@@ -457,3 +548,58 @@ class Gem:
 
     def sync(self):
         gem_sync(self.h)
+
+
+class Ops:
+    """Owns one gem_ops_t.  Arguments as in include/gem.h; addresses as integers."""
+
+    def __init__(self, scratch_bytes: int = 0, stream: int | None = None):
+        self.h = gem_ops_create(scratch_bytes, stream)
+
+    def close(self):
+        if self.h:
+            gem_ops_destroy(self.h)
+            self.h = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def token_scores(self, data, rows, vocab, dtype, stride=0, temperature=1.0, tokens=None,
+                     n_tokens=0, top_k=0, logprob=None, entropy=None, lse=None, top_ids=None,
+                     top_logprob=None):
+        z = gem_logits(data, rows, stride, vocab, dtype, temperature, 0)
+        gem_token_scores(self.h, z, tokens, n_tokens, top_k,
+                         gem_scores(logprob, entropy, lse, top_ids, top_logprob))
+
+    def distill_loss(self, data, rows, vocab, dtype, ids, teacher, k, loss, stride=0,
+                     temperature=1.0, tail=0, weight=None):
+        gem_distill_loss(self.h, gem_logits(data, rows, stride, vocab, dtype, temperature, 0),
+                         gem_teacher(ids, teacher, k, tail), weight, loss)
+
+    def distill_grad(self, data, rows, vocab, dtype, ids, teacher, k, grad, loss=None, stride=0,
+                     temperature=1.0, tail=0, weight=None, grad_stride=0):
+        gem_distill_grad(self.h, gem_logits(data, rows, stride, vocab, dtype, temperature, 0),
+                         gem_teacher(ids, teacher, k, tail), weight, loss, grad, grad_stride)
+
+    def scan_forward(self, x, gate, tokens, channels, sequences, dtype, y, offsets=None, h0=None,
+                     h_last=None, states=None, x_stride=0, gate_stride=0, y_stride=0):
+        s = gem_scan(x, gate, offsets, h0, tokens, x_stride, gate_stride, channels, sequences,
+                     dtype, 0)
+        gem_scan_forward(self.h, s, y, y_stride, h_last, states)
+
+    def scan_backward(self, x, gate, tokens, channels, sequences, dtype, states, dy, dx, dgate,
+                      offsets=None, h0=None, dh_last=None, dh0=None, x_stride=0, gate_stride=0,
+                      dy_stride=0, dx_stride=0, dgate_stride=0):
+        s = gem_scan(x, gate, offsets, h0, tokens, x_stride, gate_stride, channels, sequences,
+                     dtype, 0)
+        gem_scan_backward(self.h, s, states, dy, dy_stride, dh_last, dx, dx_stride, dgate,
+                          dgate_stride, dh0)

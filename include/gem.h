@@ -425,7 +425,7 @@ int gem_copy_f32(const float* src, float* dst, int64_t count, void* stream);
 typedef struct gem_ops_handle gem_ops_t;
 
 /* Largest vocabulary, and the most alternatives of a row. */
-#define GEM_VOCAB_MAX (1 << 24)
+#define GEM_VOCAB_MAX (1 << 22)
 #define GEM_TOP_MAX 128
 
 /* Create the handle on the current device.  stream is the hipStream_t its work

@@ -1,212 +1,892 @@
 // gem_logits.hip -- scores of rows of logits, and the distillation loss with its
-// gradient, for gfx950.  A block takes one row.
+// gradient, for gfx950.
+//
+// A row of a large vocabulary is read once: every thread keeps a sum of exponentials
+// about a reference of its own, which only moves when a logit lies 20 octaves above
+// it (the sums stay far from overflow, and no running maximum is carried from element
+// to element).  Bytes of logits bound it, and the vector instructions of an element
+// come close: an exponential, two fused multiply-adds, an addition, a conversion and
+// half a maximum.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include "gem_ops.hpp"
+#include "gem_ops_device.hpp"
 
 namespace gemk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kLn2 = 0.693147180559945309417f;
-constexpr float kInf = __builtin_inff();
+constexpr int kWaves = kThreads / 64;
+constexpr int kUnroll = 4;                 // vectors of a thread in flight, twice
 
-__device__ __forceinline__ float load(const float* p, int64_t i) { return p[i]; }
-__device__ __forceinline__ float load(const uint16_t* p, int64_t i)
-{
-    return __uint_as_float(static_cast<uint32_t>(p[i]) << 16);
-}
-__device__ __forceinline__ void store(float* p, int64_t i, float v) { p[i] = v; }
-__device__ __forceinline__ void store(uint16_t* p, int64_t i, float v)
-{
-    const uint32_t b = __float_as_uint(v);
-    // nearest even; a NaN keeps a mantissa bit
-    p[i] = static_cast<uint16_t>(v != v ? (b >> 16) | 0x40u : (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16);
-}
+// ---- running sums of exponentials -----------------------------------------------
 
-template <class F>
-__device__ float block_reduce(float v, float* lds, F f)
-{
-    __syncthreads();
-    lds[threadIdx.x] = v;
-    __syncthreads();
-    for (int s = kThreads / 2; s > 0; s >>= 1) {
-        if (threadIdx.x < s) lds[threadIdx.x] = f(lds[threadIdx.x], lds[threadIdx.x + s]);
-        __syncthreads();
+// 2^d is zero long before this.
+constexpr float kLeast = -200.0f;
+
+// Where exponents (x - ref) scale are taken from.  Fused, they are x scale - rc with
+// rc = ref scale rounded, which puts them all off by the rounding's error, skew: sums are
+// freed of it when they are moved to another reference.  Near the type's ends (a row
+// masked by the lowest value) a logit's own multiple overflows: there (wide) the
+// difference comes first.
+struct Reference {
+    float ref = -kInf, rc = 0.0f;
+    bool wide = false;
+
+    __device__ void set(float at, float scale)
+    {
+        ref = at;
+        rc = at * scale;
+        wide = !(__builtin_fabsf(rc) < 0x1p120f);
     }
-    return lds[0];
-}
+    __device__ float skew(float scale) const
+    {
+        return wide || ref == -kInf ? 0.0f : __builtin_fmaf(ref, scale, -rc);
+    }
+    __device__ float exponent(float x, float scale) const
+    {
+        return wide ? (x - ref) * scale : __builtin_fmaf(x, scale, -rc);
+    }
+};
 
-__device__ float add(float a, float b) { return a + b; }
-__device__ float most(float a, float b) { return __builtin_fmaxf(a, b); }
-
-// The order of alternatives as an integer's: logits rising, equal ones (the two
-// zeros are equal) by falling token.  0 is no alternative.
-__device__ __forceinline__ uint64_t rank_key(float v, uint32_t token)
-{
-    if (!(v > -kInf)) return 0;
-    const uint32_t b = __float_as_uint(v == 0.0f ? 0.0f : v);
-    const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
-    return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~token);
-}
-
-template <class T>
-__global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a)
-{
-    __shared__ float lds[kThreads];
-    __shared__ uint64_t keys[kThreads];
-    const int64_t r = blockIdx.x;
-    const T* row = static_cast<const T*>(a.l.z) + r * a.l.stride;
-    const int V = a.l.vocab;
-    float m = -kInf;
-    for (int v = threadIdx.x; v < V; v += kThreads) m = __builtin_fmaxf(m, load(row, v));
-    m = block_reduce(m, lds, most);
-    // Differences are taken before they are scaled: scaled on its own, a logit near the
-    // type's lowest value (a mask's) would overflow.
-    if (m == -kInf) m = 0.0f;
+// A thread's s = sum 2^d and beside it t: sum 2^d d (SUM_D), or a second sum of
+// exponentials.
+struct Run {
+    Reference at;
+    float limit = -kInf;       // a logit above it moves the reference
     float s = 0.0f, t = 0.0f;
-    for (int v = threadIdx.x; v < V; v += kThreads) {
-        const float d = (load(row, v) - m) * a.l.scale;
+};
+
+// Sums moved so that every d grows by d.
+template <bool SUM_D>
+__device__ __forceinline__ void shift_sums(float& s, float& t, float d)
+{
+    d = __builtin_fmaxf(d, kLeast);
+    const float c = __builtin_amdgcn_exp2f(d);
+    if constexpr (SUM_D) t = c * __builtin_fmaf(s, d, t);
+    else t *= c;
+    s *= c;
+}
+
+template <bool SUM_D>
+__device__ __forceinline__ void rebase(Run& r, float ref, float scale, float reach)
+{
+    const Reference from = r.at;
+    r.at.set(ref, scale);
+    r.limit = ref + reach;
+    if (from.ref > -kInf)      // else nothing is summed but zeros and NaN
+        shift_sums<SUM_D>(r.s, r.t, (from.ref - ref) * scale + (r.at.skew(scale) - from.skew(scale)));
+}
+
+template <bool SUM_D, int N>
+__device__ __forceinline__ void add(Run& r, const float (&x)[N], float most, float scale, float reach)
+{
+    if (most > r.limit) rebase<SUM_D>(r, most, scale, reach);
+    const auto sum = [&](float d) {
         const float e = __builtin_amdgcn_exp2f(d);
-        s += e;
-        t = __builtin_fmaf(e, __builtin_fmaxf(d, -200.0f), t);
+        r.s += e;
+        if constexpr (SUM_D) r.t = __builtin_fmaf(e, __builtin_fmaxf(d, kLeast), r.t);
+    };
+    if (!r.at.wide) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum(__builtin_fmaf(x[i], scale, -r.at.rc));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum((x[i] - r.at.ref) * scale);
     }
-    s = block_reduce(s, lds, add);
-    t = block_reduce(t, lds, add);
-    const float ls = __builtin_log2f(s);
+}
+
+// A row's (or a part's) sums about the largest of its references; ref is 0 where
+// no logit is above -inf.
+struct Sums {
+    float ref, s, t;
+};
+
+template <bool SUM_D>
+__device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*lds)[4])
+{
+    const float top = wave_max(r.at.ref);
+    float s = r.s, t = r.t;
+    if (r.at.ref > -kInf) shift_sums<SUM_D>(s, t, (r.at.ref - top) * scale - r.at.skew(scale));
+    s = wave_sum(s);
+    t = wave_sum(t);
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+        lds[wave][0] = top;
+        lds[wave][1] = s;
+        lds[wave][2] = t;
+    }
+    __syncthreads();
+    Sums out{lds[0][0], 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) out.ref = __builtin_fmaxf(out.ref, lds[w][0]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        s = lds[w][1];
+        t = lds[w][2];
+        if (lds[w][0] > -kInf) shift_sums<SUM_D>(s, t, (lds[w][0] - out.ref) * scale);
+        out.s += s;
+        out.t += t;
+    }
+    if (out.ref == -kInf) out.ref = 0.0f;
+    return out;
+}
+
+__device__ __forceinline__ float block_sum(float v, float* lds)
+{
+    v = wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v += lds[w];
+    return v;
+}
+
+__device__ __forceinline__ float block_max(float v, float* lds)
+{
+    v = wave_max(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v = __builtin_fmaxf(v, lds[w]);
+    return v;
+}
+
+// ---- a part of a row ----------------------------------------------------------------
+
+// Elements [begin, begin + n) of a row: up to a vector less one before the first
+// aligned address (the head), whole aligned vectors, and a tail.
+template <class T> struct Part {
+    const T* p;
+    int begin, n, head, nvec, tail;
+
+    __device__ Part(const T* row, int vocab, int begin_, int len)
+        : p(row + begin_), begin(begin_), n(vocab - begin_ < len ? vocab - begin_ : len)
+    {
+        const int off = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
+        head = (kVec<T> - off) & (kVec<T> - 1);
+        if (head > n) head = n;
+        nvec = (n - head) / kVec<T>;
+        tail = n - head - nvec * kVec<T>;
+    }
+    __device__ const u32x4* body() const { return reinterpret_cast<const u32x4*>(p + head); }
+    // The element index (from begin) at which the head (of thread 0) or the tail (of
+    // thread 1) starts, and its length.
+    __device__ int edge_at() const { return threadIdx.x == 0 ? 0 : head + nvec * kVec<T>; }
+    __device__ int edge_n() const { return threadIdx.x == 0 ? head : threadIdx.x == 1 ? tail : 0; }
+    __device__ void edge(float (&x)[kVec<T>]) const
+    {
+        const int at = edge_at(), m = edge_n();
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) x[i] = i < m ? load(p, at + i) : -kInf;
+    }
+};
+
+template <int N> __device__ __forceinline__ float most_of(const float (&x)[N])
+{
+    float m = __builtin_fmaxf(x[0], x[1]);
+#pragma unroll
+    for (int i = 2; i < N; i += 2) m = __builtin_fmaxf(__builtin_fmaxf(m, x[i]), x[i + 1]);
+    return m;
+}
+
+// f(v, vector, inside) for each vector v of the part, kUnroll loads ahead.  inside is
+// false past the end, where the last vector is given again.
+template <class F>
+__device__ __forceinline__ void stream(const u32x4* body, int nvec, F f)
+{
+    if (nvec == 0) return;
+    const int tid = threadIdx.x, last = nvec - 1;
+    u32x4 next[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int v = tid + u * kThreads;
+        next[u] = body[v < last ? v : last];
+    }
+    for (int base = 0; base < nvec; base += kThreads * kUnroll) {
+        u32x4 cur[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) cur[u] = next[u];
+        if (base + kThreads * kUnroll < nvec) {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int v = base + tid + (kUnroll + u) * kThreads;
+                next[u] = body[v < last ? v : last];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int v = base + tid + u * kThreads;
+            f(v, cur[u], v < nvec);
+        }
+    }
+}
+
+// ---- alternatives ----------------------------------------------------------------
+
+// The order of logits as an integer's (the two zeros are equal); 0 for -inf and NaN,
+// which are no alternatives.
+__device__ __forceinline__ uint32_t order(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    const uint32_t o = b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+    return v > -kInf ? o : 0u;
+}
+__device__ __forceinline__ float ordered(uint32_t o)
+{
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+// Larger logits first, of equal ones the lower token.
+__device__ __forceinline__ uint64_t rank_key(uint32_t o, uint32_t token)
+{
+    return o ? (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~token) : 0;
+}
+__device__ __forceinline__ int key_token(uint64_t key) { return static_cast<int>(~static_cast<uint32_t>(key)); }
+
+// The k largest of a row lie in the k groups of eight whose largest elements rank
+// highest (each group ahead of another has an element that ranks ahead of all of the
+// other's).  So the pass over the row keeps one key a group in LDS, and only k groups
+// are looked at again.  bfloat16 logits need 16 bits of a key.
+constexpr int kGroup = 8;
+template <class T> struct GroupKey;
+template <> struct GroupKey<uint16_t> {
+    using Type = uint16_t;
+    static constexpr int kShift = 16;      // key = order >> kShift
+};
+template <> struct GroupKey<float> {
+    using Type = uint32_t;
+    static constexpr int kShift = 0;
+};
+// Elements of a part: 32 KiB of group keys.
+template <class T> constexpr int kPartMax = (32 << 10) / static_cast<int>(sizeof(typename GroupKey<T>::Type)) * kGroup;
+
+constexpr int kList = 1024;                // GEM_TOP_MAX groups of kGroup
+static_assert(kList >= GEM_TOP_MAX * kGroup, "a group's elements fit");
+
+struct TopLds {
+    uint64_t list[kList];
+    uint64_t sel[GEM_TOP_MAX];
+    uint32_t high[kThreads];
+    int wave[2][kWaves];
+    int count;
+};
+
+__device__ __forceinline__ void push(TopLds& l, uint64_t key)
+{
+    const int at = atomicAdd(&l.count, 1);
+    if (at < kList) l.list[at] = key;
+}
+
+// The n keys of list in falling order into out, the first k of them.  All keys are
+// different, so a key's rank is the number of larger ones.
+__device__ __forceinline__ void rank_list(TopLds& l, int n, int k, uint64_t* out)
+{
+    for (int c = threadIdx.x; c < n; c += kThreads) {
+        const uint64_t mine = l.list[c];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += l.list[j] > mine;
+        if (rank < k) out[rank] = mine;
+    }
+}
+
+// A bound below which no key is among the k largest: the list of keys at or above it
+// has at least k (or all that are not 0), and at most `fit`.  key(j) gives the j-th of
+// this thread's `mine` keys.
+template <class F>
+__device__ uint64_t bound_of(TopLds& l, int mine, int k, int fit, F key)
+{
+    uint64_t bound = 0;
+    int turn = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t trial = bound | (uint64_t{1} << bit);
+        int n = 0;
+        for (int j = 0; j < mine; ++j) n += key(j) >= trial;
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) n += __shfl_xor(n, m);
+        if ((threadIdx.x & 63) == 0) l.wave[turn][threadIdx.x >> 6] = n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) n += l.wave[turn][w];
+        turn ^= 1;
+        if (n >= k) {
+            bound = trial;
+            if (n <= fit) break;
+        }
+    }
+    return bound ? bound : 1;
+}
+
+// The part's k largest logits as keys in l.sel (0 where there are fewer).  keys holds
+// a key for the head, for each group of the body, and for the tail; high is the
+// largest key of this thread's elements, seen the largest that it put there.
+template <class T>
+__device__ void select_top(TopLds& l, const Part<T>& part, const typename GroupKey<T>::Type* keys, int groups,
+                           uint32_t high, uint32_t seen, int k)
+{
+    constexpr int shift = GroupKey<T>::kShift;
+    const int tid = threadIdx.x, lane = tid & 63;
+    l.high[tid] = high;
+    if (tid == 0) l.count = 0;
+    __syncthreads();
+    // A first bound: the k-th of the threads' largest elements (16 bits of their keys).
+    uint32_t q[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) q[w] = l.high[lane + 64 * w];
+    uint32_t low = 0;
+#pragma unroll 1
+    for (int bit = 31 - shift; bit >= 16 - shift; --bit) {
+        const uint32_t trial = low | (1u << bit);
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) n += __builtin_popcountll(__ballot(q[w] >= trial));
+        if (n >= k) low = trial;
+    }
+    if (low == 0) low = 1;
+    // Each thread looks through the groups that it put there: group g of the body (key
+    // 1 + g) begins with the vector of thread g * kLanes % kThreads.
+    constexpr int kLanes = kGroup / kVec<T>;
+    if (seen >= low && tid % kLanes == 0)
+        for (int g = 1 + tid / kLanes; g < groups - 1; g += kThreads / kLanes) {
+            const uint32_t o = keys[g];
+            if (o >= low) push(l, (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~g));
+        }
+    if (tid < 2) {
+        const int g = tid == 0 ? 0 : groups - 1;
+        const uint32_t o = keys[g];
+        if (o >= low) push(l, (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~g));
+    }
+    __syncthreads();
+    int n = l.count;
+    if (n > kList) {
+        // Many equal groups: a bound that leaves few enough.
+        const auto key = [&](int j) {
+            const int g = tid + j * kThreads;
+            const uint32_t o = keys[g];
+            return o ? (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~g) : uint64_t{0};
+        };
+        const int mine = tid < groups ? (groups - tid + kThreads - 1) / kThreads : 0;
+        const uint64_t bound = bound_of(l, mine, k, kList, key);
+        __syncthreads();
+        if (tid == 0) l.count = 0;
+        __syncthreads();
+        for (int j = 0; j < mine; ++j)
+            if (key(j) >= bound) push(l, key(j));
+        __syncthreads();
+        n = l.count;
+    }
+    rank_list(l, n, k, l.sel);
+    __syncthreads();
+    if (tid == 0) l.count = 0;
+    const int picked = n < k ? n : k;
+    const uint32_t least = picked == k ? static_cast<uint32_t>(l.sel[k - 1] >> 32) : 1u;
+    __syncthreads();
+    for (int j = tid; j < picked * kGroup; j += kThreads) {
+        const int g = static_cast<int>(~static_cast<uint32_t>(l.sel[j / kGroup])), i = j % kGroup;
+        const int end = part.head + part.nvec * kVec<T>;
+        const int at = g == 0 ? i : g == groups - 1 ? end + i : part.head + (g - 1) * kGroup + i;
+        const int stop = g == 0 ? part.head : g == groups - 1 ? part.n : end;
+        if (at < stop) {
+            const uint32_t o = order(load(part.p, at));
+            if ((o >> shift) >= least) push(l, rank_key(o, static_cast<uint32_t>(part.begin + at)));
+        }
+    }
+    __syncthreads();
+    n = l.count;
+    if (tid < k) l.sel[tid] = 0;
+    __syncthreads();
+    rank_list(l, n, k, l.sel);
+    __syncthreads();
+}
+
+// ---- scores -------------------------------------------------------------------------
+
+// What a part of a row leaves for the row's joining block.
+struct PartSums {
+    float ref, s, t, pad;
+};
+
+__device__ __forceinline__ float log_prob(const LogitArgs& a, float x, float ref, float ls)
+{
+    return x == -kInf ? x : (x - ref) * a.inv_t - ls * kLn2;
+}
+
+// A row's outputs from its sums and its alternatives' keys.
+template <class T>
+__device__ void write_scores(const ScoreArgs& a, int64_t r, const T* row, const Sums& u, const uint64_t* top)
+{
+    const float ls = __builtin_log2f(u.s);
     if (threadIdx.x == 0) {
-        if (a.out.lse) a.out.lse[r] = m * a.l.inv_t + ls * kLn2;
-        if (a.out.entropy) a.out.entropy[r] = s == 0.0f ? 0.0f : (ls - t / s) * kLn2;
+        if (a.out.lse) a.out.lse[r] = u.ref * a.l.inv_t + ls * kLn2;
+        if (a.out.entropy) a.out.entropy[r] = u.s == 0.0f ? 0.0f : (ls - u.t / u.s) * kLn2;
     }
     for (int i = threadIdx.x; i < a.n_tokens; i += kThreads) {
         const int token = a.tokens[r * a.n_tokens + i];
         float lp = 0.0f;
-        if (token >= 0 && token < V) {
-            const float x = load(row, token);
-            lp = x == -kInf ? x : (x - m) * a.l.inv_t - ls * kLn2;
-        }
+        if (token >= 0 && token < a.l.vocab) lp = log_prob(a.l, load(row, token), u.ref, ls);
         a.out.logprob[r * a.n_tokens + i] = lp;
     }
-    uint64_t below = ~uint64_t{0};
-    for (int i = 0; i < a.top_k; ++i) {
-        uint64_t best = 0;
-        for (int v = threadIdx.x; v < V; v += kThreads) {
-            const uint64_t k = rank_key(load(row, v), v);
-            if (k < below && k > best) best = k;
-        }
-        __syncthreads();
-        keys[threadIdx.x] = best;
-        __syncthreads();
-        for (int h = kThreads / 2; h > 0; h >>= 1) {
-            if (threadIdx.x < h && keys[threadIdx.x + h] > keys[threadIdx.x])
-                keys[threadIdx.x] = keys[threadIdx.x + h];
-            __syncthreads();
-        }
-        below = keys[0];
-        if (threadIdx.x == 0) {
-            const int token = below ? static_cast<int>(~static_cast<uint32_t>(below)) : -1;
-            if (a.out.top_ids) a.out.top_ids[r * a.top_k + i] = token;
-            if (a.out.top_logprob)
-                a.out.top_logprob[r * a.top_k + i] =
-                    below ? (load(row, token) - m) * a.l.inv_t - ls * kLn2 : -kInf;
-        }
+    for (int i = threadIdx.x; i < a.top_k; i += kThreads) {
+        const uint64_t key = top[i];
+        if (a.out.top_ids) a.out.top_ids[r * a.top_k + i] = key ? key_token(key) : -1;
+        if (a.out.top_logprob)
+            a.out.top_logprob[r * a.top_k + i] =
+                key ? log_prob(a.l, ordered(static_cast<uint32_t>(key >> 32)), u.ref, ls) : -kInf;
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a)
+// One part of one row a block.  A whole row is written out; parts leave their sums
+// and keys for join_kernel.
+template <class T, bool TOP>
+__global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a, int64_t row0, int parts, int len,
+                                                         PartSums* sums, uint64_t* tops)
 {
-    __shared__ float lds[kThreads];
-    __shared__ int ids[GEM_TOP_MAX];
-    const int64_t r = blockIdx.x;
+    using Key = typename GroupKey<T>::Type;
+    constexpr int shift = GroupKey<T>::kShift;
+    extern __shared__ uint32_t dynamic_lds[];
+    Key* keys = reinterpret_cast<Key*>(dynamic_lds);
+    __shared__ float lds[kWaves][4];
+    __shared__ TopLds top;
+    const int64_t r = row0 + blockIdx.x / parts;
+    const int q = blockIdx.x % parts, tid = threadIdx.x;
     const T* row = static_cast<const T*>(a.l.z) + r * a.l.stride;
-    T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
-    const int V = a.l.vocab, tid = threadIdx.x;
-    const float w = a.weight ? a.weight[r] : 1.0f;
-    if (w == 0.0f) {
-        if (tid == 0 && a.loss) a.loss[r] = 0.0f;
-        if (grad)
-            for (int v = tid; v < V; v += kThreads) store(grad, v, 0.0f);
-        return;
+    const Part<T> part(row, a.l.vocab, q * len, len);
+    const float scale = a.l.scale, reach = 20.0f / scale;
+    const int groups = (part.nvec * kVec<T> + kGroup - 1) / kGroup + 2;
+    Run run;
+    uint32_t high = 0, seen = 0;   // largest key of the thread's elements, and of its groups
+    if (tid < 64) {
+        float x[kVec<T>];
+        part.edge(x);
+        const float m = most_of(x);
+        add<true>(run, x, m, scale, reach);
+        if constexpr (TOP)
+            if (tid < 2) {
+                high = seen = order(m) >> shift;
+                keys[tid == 0 ? 0 : groups - 1] = static_cast<Key>(high);
+            }
     }
+    stream(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
+        float x[kVec<T>];
+        unpack(raw, x);
+        float m = most_of(x);
+        if constexpr (TOP) {
+            float both = inside ? m : -kInf;
+            if constexpr (kVec<T> < kGroup) both = __builtin_fmaxf(both, __shfl_xor(both, 1));
+            const uint32_t o = order(both) >> shift;
+            seen = o > seen ? o : seen;
+            if constexpr (kVec<T> < kGroup) {
+                const uint32_t own = inside ? order(m) >> shift : 0;
+                high = own > high ? own : high;
+                if (inside && (v & 1) == 0) keys[1 + v / 2] = static_cast<Key>(o);
+            } else {
+                high = seen;
+                if (inside) keys[1 + v] = static_cast<Key>(o);
+            }
+        }
+        if (inside) add<true>(run, x, m, scale, reach);
+    });
+    const Sums u = block_sums<true>(run, scale, lds);
+    if constexpr (TOP) select_top(top, part, keys, groups, high, seen, a.top_k);
+    if (parts == 1) {
+        write_scores(a, r, row, u, top.sel);
+    } else {
+        if (tid == 0) sums[blockIdx.x] = PartSums{u.s == 0.0f ? -kInf : u.ref, u.s, u.t, 0.0f};
+        if constexpr (TOP)
+            if (tid < a.top_k) tops[static_cast<int64_t>(blockIdx.x) * a.top_k + tid] = top.sel[tid];
+    }
+}
+
+// A row's parts joined (parts <= kPartsMax).
+constexpr int kPartsMax = 64;
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void join_kernel(const ScoreArgs a, int64_t row0, int parts,
+                                                        const PartSums* sums, const uint64_t* tops)
+{
+    extern __shared__ uint32_t dynamic_lds[];
+    uint64_t* keys = reinterpret_cast<uint64_t*>(dynamic_lds);
+    __shared__ float lds[kWaves][4];
+    __shared__ TopLds top;
+    const int64_t r = row0 + blockIdx.x;
+    const int tid = threadIdx.x;
+    const T* row = static_cast<const T*>(a.l.z) + r * a.l.stride;
+    Run run;
+    if (tid < parts) {
+        const PartSums p = sums[static_cast<int64_t>(blockIdx.x) * parts + tid];
+        run.at.ref = p.ref;    // its sums have no skew
+        run.at.wide = true;
+        run.s = p.s;
+        run.t = p.t;
+    }
+    const int n = parts * a.top_k;
+    for (int j = tid; j < n; j += kThreads) keys[j] = tops[static_cast<int64_t>(blockIdx.x) * n + j];
+    if (tid == 0) top.count = 0;
+    const Sums u = block_sums<true>(run, a.l.scale, lds);
+    if (a.top_k) {
+        const int mine = tid < n ? (n - tid + kThreads - 1) / kThreads : 0;
+        const auto key = [&](int j) { return keys[tid + j * kThreads]; };
+        const uint64_t bound = bound_of(top, mine, a.top_k, kThreads, key);
+        for (int j = 0; j < mine; ++j)
+            if (key(j) >= bound) push(top, key(j));
+        if (tid < a.top_k) top.sel[tid] = 0;
+        __syncthreads();
+        rank_list(top, top.count, a.top_k, top.sel);
+        __syncthreads();
+    }
+    write_scores(a, r, row, u, top.sel);
+}
+
+// ---- distillation ----------------------------------------------------------------
+
+struct DistillLds {
+    float sums[kWaves][4];
+    float red[kWaves];
+    int ids[GEM_TOP_MAX];
+};
+
+// Thread i's entry of the row's record: its token (-1: none), log probability and
+// probability, and p_t.
+struct Teacher {
     int id = -1;
+    float lp = 0.0f, p = 0.0f, pt = 0.0f;
+};
+
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, int64_t r, DistillLds& l)
+{
+    Teacher t;
+    const int tid = threadIdx.x;
+    float lp = -kInf;
     if (tid < a.k) {
-        id = a.ids[r * a.k + tid];
-        if (id < 0 || id >= V) id = -1;
-        ids[tid] = id;
+        t.id = a.ids[r * a.k + tid];
+        lp = a.lp[r * a.k + tid];
+        if (t.id < 0 || t.id >= a.l.vocab) t.id = -1;
+        l.ids[tid] = t.id;
     }
     __syncthreads();
     if (tid < a.k)
         for (int i = 0; i < tid; ++i)
-            if (ids[i] == id) id = -1;
-    float m = -kInf;
-    for (int v = tid; v < V; v += kThreads) m = __builtin_fmaxf(m, load(row, v));
-    m = block_reduce(m, lds, most);
-    // Differences are taken before they are scaled: scaled on its own, a logit near the
-    // type's lowest value (a mask's) would overflow.
-    if (m == -kInf) m = 0.0f;
-    float lp = id >= 0 ? a.lp[r * a.k + tid] : -kInf;
-    float p, lse_p = 0.0f;
+            if (l.ids[i] == t.id) t.id = -1;
+    if (t.id < 0) lp = -kInf;
     if (a.tail) {
-        p = id >= 0 ? expf(lp) : 0.0f;
+        t.lp = lp;
+        t.p = t.id >= 0 ? expf(lp) : 0.0f;
+        t.pt = __builtin_fmaxf(0.0f, 1.0f - block_sum(t.p, l.red));
     } else {
-        const float top = block_reduce(lp, lds, most);
-        p = id >= 0 && top > -kInf ? expf(lp - top) : 0.0f;
-        const float sum = block_reduce(p, lds, add);
-        p = sum > 0.0f ? p / sum : 0.0f;
-        lse_p = top + logf(sum);
+        const float top = block_max(lp, l.red);
+        t.p = t.id >= 0 && top > -kInf ? expf(lp - top) : 0.0f;
+        const float sum = block_sum(t.p, l.red);
+        t.lp = lp - (top + logf(sum));
+        t.p = sum > 0.0f ? t.p / sum : 0.0f;
     }
-    const float pt = a.tail ? __builtin_fmaxf(0.0f, 1.0f - block_reduce(p, lds, add)) : 0.0f;
-    const float x = id >= 0 ? load(row, id) : 0.0f;
-    const float d = (x - m) * a.l.scale;
-    float s_all = 0.0f, s_out = 0.0f;
-    if (tid < a.k) ids[tid] = id;
-    __syncthreads();
-    for (int v = tid; v < V; v += kThreads) {
-        const float e = __builtin_amdgcn_exp2f((load(row, v) - m) * a.l.scale);
-        s_all += e;
-        bool listed = false;
-        for (int i = 0; i < a.k; ++i) listed |= ids[i] == v;
-        if (!listed) s_out += e;
+    return t;
+}
+
+// Marks of the part's listed tokens: a bit for each element of each vector, a vector's
+// bits where its thread finds those of its kUnroll vectors in one word.
+__device__ __forceinline__ int mark_byte(int v)
+{
+    constexpr int kRound = kThreads * kUnroll;
+    return v / kRound * kRound + v % kThreads * kUnroll + v % kRound / kThreads;
+}
+
+template <class T>
+__device__ __forceinline__ void mark(const Part<T>& part, uint8_t* marks, uint32_t* edges, int id)
+{
+    const int at = id - part.begin;
+    if (id < 0 || at < 0 || at >= part.n) return;
+    const int end = part.head + part.nvec * kVec<T>;
+    if (at < part.head) {
+        atomicOr(&edges[0], 1u << at);
+    } else if (at >= end) {
+        atomicOr(&edges[1], 1u << (at - end));
+    } else {
+        const int v = (at - part.head) / kVec<T>, byte = mark_byte(v);
+        atomicOr(reinterpret_cast<uint32_t*>(marks) + byte / 4,
+                 1u << (byte % 4 * 8 + (at - part.head) % kVec<T>));
     }
-    s_all = block_reduce(s_all, lds, add);
-    s_out = block_reduce(s_out, lds, add);
-    const float ls = __builtin_log2f(s_all);
+}
+
+__host__ __device__ constexpr int mark_words(int nvec)
+{
+    return (nvec + kThreads * kUnroll - 1) / (kThreads * kUnroll) * kThreads;
+}
+
+// The part's sums over unlisted tokens (s) and listed ones (t).  Without marks every
+// token counts as unlisted.
+template <class T, bool MARKS>
+__device__ __forceinline__ Sums distill_sums(const DistillArgs& a, const Part<T>& part, const uint32_t* marks,
+                                             const uint32_t* edges, DistillLds& l)
+{
+    const float scale = a.l.scale, reach = 20.0f / scale;
+    Run run;
+    const auto take = [&](float (&x)[kVec<T>], uint32_t listed) {
+        const float m = most_of(x);
+        if (MARKS && listed) {
+            if (m > run.limit) rebase<false>(run, m, scale, reach);
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) {
+                const float e = __builtin_amdgcn_exp2f(run.at.exponent(x[i], scale));
+                if (listed >> i & 1u) run.t += e;
+                else run.s += e;
+            }
+        } else {
+            add<false>(run, x, m, scale, reach);
+        }
+    };
+    if (threadIdx.x < 64) {
+        float x[kVec<T>];
+        part.edge(x);
+        take(x, MARKS && threadIdx.x < 2 ? edges[threadIdx.x] : 0u);
+    }
+    stream(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
+        if (!inside) return;
+        float x[kVec<T>];
+        unpack(raw, x);
+        uint32_t listed = 0;
+        if constexpr (MARKS) listed = reinterpret_cast<const uint8_t*>(marks)[mark_byte(v)];
+        take(x, listed);
+    });
+    return block_sums<false>(run, scale, l.sums);
+}
+
+// The row's loss, from thread i's entry and its logit.
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t, float x, const Sums& u, DistillLds& l)
+{
+    const float all = u.s + u.t, ls = __builtin_log2f(all);
     float part = 0.0f;
-    if (p > 0.0f) part = p * (lp - lse_p - (x == -kInf ? x : (x - m) * a.l.inv_t - ls * kLn2));
-    float loss = block_reduce(part, lds, add);
-    if (pt > 0.0f)
-        loss += s_out == 0.0f ? kInf : pt * (logf(pt) - (__builtin_log2f(s_out) - ls) * kLn2);
-    if (tid == 0 && a.loss) a.loss[r] = loss;
-    if (!grad) return;
-    const float f = w * a.l.inv_t;
-    const float inv = s_all == 0.0f ? 0.0f : 1.0f / s_all;
-    const float rest = pt > 0.0f && s_out != 0.0f ? pt / s_out : 0.0f;
-    for (int v = tid; v < V; v += kThreads) {
-        const float e = __builtin_amdgcn_exp2f((load(row, v) - m) * a.l.scale);
-        store(grad, v, f * (e * (inv - rest)));
+    if (t.p > 0.0f) part = t.p * (t.lp - log_prob(a.l, x, u.ref, ls));
+    float loss = block_sum(part, l.red);
+    if (t.pt > 0.0f)
+        loss += u.s == 0.0f ? kInf : t.pt * (logf(t.pt) - (__builtin_log2f(u.s) - ls) * kLn2);
+    return loss;
+}
+
+// The part's gradient: every token by the unlisted tokens' form, then the listed.
+template <class T>
+__device__ __forceinline__ void write_grad(const DistillArgs& a, const Part<T>& part, T* grad, const Teacher& t, float x,
+                                           const Sums& u, float w)
+{
+    const float scale = a.l.scale, f = w * a.l.inv_t;
+    const float all = u.s + u.t;
+    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+    const float rest = t.pt > 0.0f && u.s != 0.0f ? t.pt / u.s : 0.0f;
+    Reference at;
+    at.set(u.ref, scale);
+    const float c = f * (inv - rest) * __builtin_amdgcn_exp2f(-at.skew(scale));
+    T* out = grad + part.begin;
+    if (threadIdx.x < 2) {
+        const int from = part.edge_at(), m = part.edge_n();
+        for (int i = from; i < from + m; ++i)
+            store(out, i, c * __builtin_amdgcn_exp2f(at.exponent(load(part.p, i), scale)));
     }
+    T* body = out + part.head;
+    // The gradient's own rows may be aligned otherwise than the logits'.
+    const bool whole = (reinterpret_cast<uintptr_t>(body) & 15u) == 0;
+    stream(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
+        if (!inside) return;
+        float y[kVec<T>];
+        unpack(raw, y);
+        if (!at.wide) {
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i)
+                y[i] = c * __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], scale, -at.rc));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) y[i] = c * __builtin_amdgcn_exp2f((y[i] - at.ref) * scale);
+        }
+        if (whole) {
+            __builtin_nontemporal_store(pack(y), reinterpret_cast<u32x4*>(body) + v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) store(body, static_cast<int64_t>(v) * kVec<T> + i, y[i]);
+        }
+    });
+    // The listed tokens' elements are stored again, behind the others.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (id >= 0) store(grad, id, f * (__builtin_amdgcn_exp2f(d) * inv - p));
+    if (t.id >= part.begin && t.id < part.begin + part.n)
+        store(grad, t.id, f * (__builtin_amdgcn_exp2f((x - at.ref) * scale) * inv - t.p));
+}
+
+template <class T>
+__device__ __forceinline__ void no_grad(const Part<T>& part, T* grad)
+{
+    T* out = grad + part.begin;
+    const int off = static_cast<int>((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(T));
+    int head = (kVec<T> - off) & (kVec<T> - 1);
+    if (head > part.n) head = part.n;
+    const int nvec = (part.n - head) / kVec<T>, end = head + nvec * kVec<T>;
+    for (int i = threadIdx.x; i < head; i += kThreads) store(out, i, 0.0f);
+    for (int i = end + threadIdx.x; i < part.n; i += kThreads) store(out, i, 0.0f);
+    for (int v = threadIdx.x; v < nvec; v += kThreads)
+        __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>(out + head) + v);
+}
+
+// What a block does with its part: sums alone (left in part_sums, and the logits of the
+// part's listed tokens in part_x, [rows][k]: the gradient may be written over the logits
+// while another part's block needs them), the rest from those, or, with one part a row, both.
+enum : int { kSums = 1, kRest = 2 };
+
+template <class T, int STEP>
+__global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a, int64_t row0, int parts, int len,
+                                                           PartSums* part_sums, float* part_x)
+{
+    extern __shared__ uint32_t dynamic_lds[];
+    __shared__ DistillLds l;
+    __shared__ uint32_t edges[2];
+    const int blocks = STEP == kRest && !a.grad ? 1 : parts;       // of a row
+    const int64_t i = blockIdx.x / blocks, r = row0 + i;
+    const int q = blockIdx.x % blocks, tid = threadIdx.x;
+    const T* row = static_cast<const T*>(a.l.z) + r * a.l.stride;
+    T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
+    const Part<T> part(row, a.l.vocab, q * len, len);
+    const float w = a.weight ? a.weight[r] : 1.0f;
+    if (w == 0.0f) {
+        if (STEP & kRest) {
+            if (tid == 0 && q == 0 && a.loss) a.loss[r] = 0.0f;
+            if (grad) no_grad(part, grad);
+        }
+        return;
+    }
+    const Teacher t = teacher_of(a, r, l);
+    Sums u{0.0f, 0.0f, 0.0f};
+    if constexpr (STEP & kSums) {
+        if (a.tail) {
+            const int words = mark_words(part.nvec);
+            for (int i = tid; i < words; i += kThreads) dynamic_lds[i] = 0;
+            if (tid < 2) edges[tid] = 0;
+            __syncthreads();
+            mark(part, reinterpret_cast<uint8_t*>(dynamic_lds), edges, t.id);
+            __syncthreads();
+            u = distill_sums<T, true>(a, part, dynamic_lds, edges, l);
+        } else {
+            u = distill_sums<T, false>(a, part, dynamic_lds, edges, l);
+        }
+        if constexpr (!(STEP & kRest)) {
+            if (tid == 0) part_sums[blockIdx.x] = PartSums{u.s + u.t == 0.0f ? -kInf : u.ref, u.s, u.t, 0.0f};
+            if (t.id >= part.begin && t.id < part.begin + part.n)
+                part_x[i * a.k + tid] = load(row, t.id);
+            return;
+        }
+    } else {
+        Run run;
+        if (tid < parts) {
+            const PartSums p = part_sums[i * parts + tid];
+            run.at.ref = p.ref;    // its sums have no skew
+            run.at.wide = true;
+            run.s = p.s;
+            run.t = p.t;
+        }
+        u = block_sums<false>(run, a.l.scale, l.sums);
+    }
+    float x = 0.0f;            // thread i's entry's logit
+    if (t.id >= 0)
+        x = STEP & kSums ? load(row, t.id) : part_x[i * a.k + tid];
+    if (a.loss && q == 0) {
+        const float loss = loss_of(a, t, x, u, l);
+        if (tid == 0) a.loss[r] = loss;
+    }
+    if (grad) {
+        __syncthreads();       // every logit of an entry is read before the part is written over
+        write_grad(a, part, grad, t, x, u, w);
+    }
+}
+
+// ---- launches ----------------------------------------------------------------------
+
+// Parts of a row: at least what the group keys' LDS asks for, and with few rows
+// enough blocks for the device, of no less than kLeastPart elements each.
+constexpr int kLeastPart = 4096;
+
+struct Split {
+    int parts, len;
+};
+
+template <class T>
+Split split_rows(int64_t rows, int vocab, int cus)
+{
+    int64_t parts = (vocab + kPartMax<T> - 1) / kPartMax<T>;
+    const int64_t want = (int64_t{3} * cus + rows - 1) / rows;
+    const int64_t most = vocab / kLeastPart > 1 ? vocab / kLeastPart : 1;
+    int64_t more = want < most ? want : most;
+    if (more > kPartsMax) more = kPartsMax;
+    if (more > parts) parts = more;
+    int len = static_cast<int>((vocab + parts - 1) / parts);
+    len = (len + 63) / 64 * 64;            // parts of aligned rows stay aligned
+    if (len > kPartMax<T>) len = kPartMax<T>;
+    return {(vocab + len - 1) / len, len};
+}
+static_assert(GEM_VOCAB_MAX / kPartMax<float> <= kPartsMax, "a row's parts are joined by one block");
+
+template <class T>
+hipError_t scores(const ScoreArgs& a, const OpsDevice& d, hipStream_t stream)
+{
+    const Split s = split_rows<T>(a.l.rows, a.l.vocab, d.cus);
+    const size_t key_bytes = (static_cast<size_t>(s.len) / kGroup + 4) * sizeof(typename GroupKey<T>::Type);
+    // Rows of one launch: what their parts leave fits the fixed scratch.
+    const int64_t left = s.parts * (static_cast<int64_t>(sizeof(PartSums)) + a.top_k * 8);
+    int64_t fit = s.parts == 1 ? a.l.rows : kFixedScratch / left;
+    PartSums* sums = static_cast<PartSums*>(d.scratch);
+    for (int64_t r = 0; r < a.l.rows; r += fit) {
+        const int64_t n = a.l.rows - r < fit ? a.l.rows - r : fit;
+        uint64_t* tops = reinterpret_cast<uint64_t*>(sums + n * s.parts);
+        const dim3 grid(static_cast<unsigned>(n * s.parts));
+        if (a.top_k)
+            hipLaunchKernelGGL((score_kernel<T, true>), grid, dim3(kThreads), key_bytes, stream, a, r, s.parts, s.len, sums, tops);
+        else
+            hipLaunchKernelGGL((score_kernel<T, false>), grid, dim3(kThreads), 0, stream, a, r, s.parts, s.len, sums, tops);
+        if (s.parts > 1)
+            hipLaunchKernelGGL((join_kernel<T>), dim3(static_cast<unsigned>(n)), dim3(kThreads),
+                               static_cast<size_t>(s.parts) * a.top_k * 8, stream, a, r, s.parts, sums, tops);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <class T>
+hipError_t distill(const DistillArgs& a, const OpsDevice& d, hipStream_t stream)
+{
+    const Split s = split_rows<T>(a.l.rows, a.l.vocab, d.cus);
+    const size_t marks = a.tail ? static_cast<size_t>(mark_words(s.len / kVec<T> + 1)) * 4 : 0;
+    PartSums* sums = static_cast<PartSums*>(d.scratch);
+    if (s.parts == 1) {
+        hipLaunchKernelGGL((distill_kernel<T, kSums | kRest>), dim3(static_cast<unsigned>(a.l.rows)), dim3(kThreads), marks,
+                           stream, a, int64_t{0}, 1, s.len, sums, nullptr);
+        return hipGetLastError();
+    }
+    const int64_t fit = kFixedScratch / (s.parts * static_cast<int64_t>(sizeof(PartSums)) + a.k * 4);
+    for (int64_t r = 0; r < a.l.rows; r += fit) {
+        const int64_t n = a.l.rows - r < fit ? a.l.rows - r : fit;
+        float* x = reinterpret_cast<float*>(sums + n * s.parts);
+        const dim3 grid(static_cast<unsigned>(n * s.parts));
+        hipLaunchKernelGGL((distill_kernel<T, kSums>), grid, dim3(kThreads), marks, stream, a, r, s.parts, s.len, sums, x);
+        // The loss alone is one block's a row.
+        const int rest = a.grad ? s.parts : 1;
+        hipLaunchKernelGGL((distill_kernel<T, kRest>), dim3(static_cast<unsigned>(n * rest)), dim3(kThreads), 0, stream, a,
+                           r, s.parts, s.len, sums, x);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
 
-hipError_t launch_scores(const ScoreArgs& a, bool bf16, hipStream_t stream)
+hipError_t launch_scores(const ScoreArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream)
 {
-    const dim3 grid(static_cast<unsigned>(a.l.rows));
-    if (bf16) hipLaunchKernelGGL((score_kernel<uint16_t>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((score_kernel<float>), grid, dim3(kThreads), 0, stream, a);
-    return hipGetLastError();
+    return bf16 ? scores<uint16_t>(a, d, stream) : scores<float>(a, d, stream);
 }
 
-hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t stream)
+hipError_t launch_distill(const DistillArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream)
 {
-    const dim3 grid(static_cast<unsigned>(a.l.rows));
-    if (bf16) hipLaunchKernelGGL((distill_kernel<uint16_t>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((distill_kernel<float>), grid, dim3(kThreads), 0, stream, a);
-    return hipGetLastError();
+    return bf16 ? distill<uint16_t>(a, d, stream) : distill<float>(a, d, stream);
 }
 
 }  // namespace gemk

@@ -10,9 +10,7 @@
 struct gem_ops_handle {
     int device = 0;
     hipStream_t stream = nullptr;
-    int32_t cus = 0;             // compute units of the device
-    void* scratch = nullptr;
-    int64_t scratch_bytes = 0;
+    gemk::OpsDevice dev{};
 };
 
 namespace {
@@ -96,18 +94,18 @@ int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out)
     o->stream = static_cast<hipStream_t>(stream);
     const int rc = [&]() -> int {
         OPS_HIP(hipGetDevice(&o->device));
-        OPS_HIP(hipDeviceGetAttribute(&o->cus, hipDeviceAttributeMultiprocessorCount, o->device));
+        OPS_HIP(hipDeviceGetAttribute(&o->dev.cus, hipDeviceAttributeMultiprocessorCount, o->device));
         if (scratch_bytes > INT64_MAX - gemk::kFixedScratch) return GEM_ENOMEM;
         const size_t bytes = static_cast<size_t>(scratch_bytes + gemk::kFixedScratch);
-        const hipError_t e = hipMalloc(&o->scratch, bytes);
+        const hipError_t e = hipMalloc(&o->dev.scratch, bytes);
         if (e != hipSuccess) {
             gemk::note_hip_error("gem_ops.cpp", "hipMalloc", e, __LINE__);
             (void)hipGetLastError();
-            o->scratch = nullptr;
+            o->dev.scratch = nullptr;
             return GEM_ENOMEM;
         }
-        o->scratch_bytes = scratch_bytes;
-        OPS_HIP(hipMemsetAsync(o->scratch, 0, bytes, o->stream));
+        o->dev.scan_bytes = scratch_bytes;
+        OPS_HIP(hipMemsetAsync(o->dev.scratch, 0, bytes, o->stream));
         OPS_HIP(hipStreamSynchronize(o->stream));
         return GEM_OK;
     }();
@@ -122,9 +120,9 @@ int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out)
 int gem_ops_destroy(gem_ops_t* ops)
 {
     if (!ops) return GEM_EINVAL;
-    if (ops->scratch) {
+    if (ops->dev.scratch) {
         (void)hipStreamSynchronize(ops->stream);
-        (void)hipFree(ops->scratch);
+        (void)hipFree(ops->dev.scratch);
     }
     delete ops;
     return GEM_OK;
@@ -147,7 +145,7 @@ int gem_token_scores(gem_ops_t* ops, const gem_logits* z, const int32_t* tokens,
     a.top_k = out->top_ids || out->top_logprob ? top_k : 0;
     a.out = *out;
     if (a.l.rows == 0) return GEM_OK;
-    OPS_HIP(gemk::launch_scores(a, z->dtype == GEM_BF16, ops->stream));
+    OPS_HIP(gemk::launch_scores(a, z->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
 }
 
@@ -172,7 +170,7 @@ static int distill(gem_ops_t* ops, const gem_logits* z, const gem_teacher* t, co
     a.loss = loss;
     a.grad = grad;
     if (a.l.rows == 0) return GEM_OK;
-    OPS_HIP(gemk::launch_distill(a, z->dtype == GEM_BF16, ops->stream));
+    OPS_HIP(gemk::launch_distill(a, z->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
 }
 

@@ -69,8 +69,15 @@ struct ScanBackArgs {
     float* dh0;
 };
 
-hipError_t launch_scores(const ScoreArgs& a, bool bf16, hipStream_t stream);
-hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t stream);
+// What a handle gives a launch.
+struct OpsDevice {
+    int32_t cus;             // compute units
+    void* scratch;           // kFixedScratch bytes, then scan_bytes
+    int64_t scan_bytes;
+};
+
+hipError_t launch_scores(const ScoreArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
+hipError_t launch_distill(const DistillArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_scan_forward(const ScanArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_scan_backward(const ScanBackArgs& a, bool bf16, hipStream_t stream);
 

@@ -39,7 +39,7 @@ GEM_SNAPSHOT, GEM_MOMENT = 0, 1
 GEM_K_MAX = 32
 GEM_P_MAX = 1 << 31
 GEM_PI_BINS = 643
-GEM_VOCAB_MAX = 1 << 24
+GEM_VOCAB_MAX = 1 << 22
 GEM_TOP_MAX = 128
 
 # Every symbol include/gem.h declares.

@@ -10,6 +10,7 @@
 struct gem_ops_handle {
     int device = 0;
     hipStream_t stream = nullptr;
+    void* memory = nullptr;
     gemk::OpsDevice dev{};
 };
 
@@ -29,6 +30,9 @@ namespace {
 // products and every byte offset formed from them stay within 63 bits.
 constexpr int64_t kRowsMax = int64_t{1} << 22;
 constexpr int64_t kTokensMax = INT32_MAX;
+// A handle's memory: counters, the fixed scratch, the recurrences' scratch.
+constexpr int64_t kCounterBytes = 256;
+constexpr int64_t kFixed = kCounterBytes + gemk::kFixedScratch;
 constexpr int64_t kStrideMax = int64_t{1} << 28;
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -74,12 +78,17 @@ int check_scan(const gem_scan* s, gem_scan* out)
     if (!row_stride(s->x_stride, s->channels, &out->x_stride)) return GEM_EINVAL;
     if (!row_stride(s->gate_stride, s->channels, &out->gate_stride)) return GEM_EINVAL;
     if (!s->offsets && s->tokens % s->sequences != 0) return GEM_EINVAL;
+    // Tiles are counted in 32 bits (arrays of so many would not fit any device).
+    if (gemk::scan_tiles(s->tokens, s->channels) > INT32_MAX) return GEM_EINVAL;
     if (s->tokens > 0 && (!s->x || !s->gate)) return GEM_EINVAL;
     if (!aligned(s->x, element(s->dtype)) || !aligned(s->gate, element(s->dtype)) ||
         !aligned(s->offsets, 8) || !aligned(s->h0, 4))
         return GEM_EALIGN;
     return GEM_OK;
 }
+
+// One token a sequence needs no scratch.
+bool single_tokens(const gem_scan& s) { return !s.offsets && s.tokens == s.sequences; }
 
 }  // namespace
 
@@ -95,17 +104,21 @@ int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out)
     const int rc = [&]() -> int {
         OPS_HIP(hipGetDevice(&o->device));
         OPS_HIP(hipDeviceGetAttribute(&o->dev.cus, hipDeviceAttributeMultiprocessorCount, o->device));
-        if (scratch_bytes > INT64_MAX - gemk::kFixedScratch) return GEM_ENOMEM;
-        const size_t bytes = static_cast<size_t>(scratch_bytes + gemk::kFixedScratch);
-        const hipError_t e = hipMalloc(&o->dev.scratch, bytes);
+        if (scratch_bytes > INT64_MAX - kFixed) return GEM_ENOMEM;
+        const size_t bytes = static_cast<size_t>(scratch_bytes + kFixed);
+        const hipError_t e = hipMalloc(&o->memory, bytes);
         if (e != hipSuccess) {
             gemk::note_hip_error("gem_ops.cpp", "hipMalloc", e, __LINE__);
             (void)hipGetLastError();
-            o->dev.scratch = nullptr;
+            o->memory = nullptr;
             return GEM_ENOMEM;
         }
+        char* base = static_cast<char*>(o->memory);
+        o->dev.counters = base;
+        o->dev.scratch = base + kCounterBytes;
+        o->dev.scan = base + kFixed;
         o->dev.scan_bytes = scratch_bytes;
-        OPS_HIP(hipMemsetAsync(o->dev.scratch, 0, bytes, o->stream));
+        OPS_HIP(hipMemsetAsync(o->memory, 0, bytes, o->stream));
         OPS_HIP(hipStreamSynchronize(o->stream));
         return GEM_OK;
     }();
@@ -120,9 +133,9 @@ int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out)
 int gem_ops_destroy(gem_ops_t* ops)
 {
     if (!ops) return GEM_EINVAL;
-    if (ops->dev.scratch) {
+    if (ops->memory) {
         (void)hipStreamSynchronize(ops->stream);
-        (void)hipFree(ops->dev.scratch);
+        (void)hipFree(ops->memory);
     }
     delete ops;
     return GEM_OK;
@@ -191,7 +204,7 @@ int gem_distill_grad(gem_ops_t* ops, const gem_logits* z, const gem_teacher* tea
 int gem_scan_scratch(int64_t tokens, int32_t channels, int64_t* bytes)
 {
     if (!bytes || tokens < 0 || tokens > kTokensMax || channels < 1) return GEM_EINVAL;
-    *bytes = 0;
+    *bytes = gemk::scan_scratch_bytes(tokens, channels);
     return GEM_OK;
 }
 
@@ -215,7 +228,9 @@ int gem_scan_forward(gem_ops_t* ops, const gem_scan* s, void* y, int64_t y_strid
     a.y = y;
     a.h_last = h_last;
     a.states = states;
-    OPS_HIP(gemk::launch_scan_forward(a, s->dtype == GEM_BF16, ops->stream));
+    if (gemk::scan_scratch_bytes(s->tokens, s->channels) > ops->dev.scan_bytes && !single_tokens(*s))
+        return GEM_ESCRATCH;
+    OPS_HIP(gemk::launch_scan_forward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
 }
 
@@ -240,7 +255,8 @@ int gem_scan_backward(gem_ops_t* ops, const gem_scan* s, const float* states, co
     a.dx = dx;
     a.dgate = dgate;
     a.dh0 = dh0;
-    OPS_HIP(gemk::launch_scan_backward(a, s->dtype == GEM_BF16, ops->stream));
+    if (gemk::scan_scratch_bytes(s->tokens, s->channels) > ops->dev.scan_bytes) return GEM_ESCRATCH;
+    OPS_HIP(gemk::launch_scan_backward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
 }
 

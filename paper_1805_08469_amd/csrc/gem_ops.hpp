@@ -72,13 +72,17 @@ struct ScanBackArgs {
 // What a handle gives a launch.
 struct OpsDevice {
     int32_t cus;             // compute units
-    void* scratch;           // kFixedScratch bytes, then scan_bytes
+    void* counters;          // 256 bytes, zero when the handle is made
+    void* scratch;           // kFixedScratch bytes
+    void* scan;              // scan_bytes bytes, zero when the handle is made
     int64_t scan_bytes;
 };
 
 hipError_t launch_scores(const ScoreArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_distill(const DistillArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
-hipError_t launch_scan_forward(const ScanArgs& a, bool bf16, hipStream_t stream);
-hipError_t launch_scan_backward(const ScanBackArgs& a, bool bf16, hipStream_t stream);
+int64_t scan_tiles(int64_t tokens, int64_t channels);
+int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);
+hipError_t launch_scan_forward(const ScanArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
+hipError_t launch_scan_backward(const ScanBackArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 
 }  // namespace gemk

@@ -30,9 +30,6 @@ namespace {
 // products and every byte offset formed from them stay within 63 bits.
 constexpr int64_t kRowsMax = int64_t{1} << 22;
 constexpr int64_t kTokensMax = INT32_MAX;
-// A handle's memory: counters, the fixed scratch, the recurrences' scratch.
-constexpr int64_t kCounterBytes = 256;
-constexpr int64_t kFixed = kCounterBytes + gemk::kFixedScratch;
 constexpr int64_t kStrideMax = int64_t{1} << 28;
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -78,8 +75,9 @@ int check_scan(const gem_scan* s, gem_scan* out)
     if (!row_stride(s->x_stride, s->channels, &out->x_stride)) return GEM_EINVAL;
     if (!row_stride(s->gate_stride, s->channels, &out->gate_stride)) return GEM_EINVAL;
     if (!s->offsets && s->tokens % s->sequences != 0) return GEM_EINVAL;
-    // Tiles are counted in 32 bits (arrays of so many would not fit any device).
-    if (gemk::scan_tiles(s->tokens, s->channels) > INT32_MAX) return GEM_EINVAL;
+    // A launch's threads, 32 a row, are counted in 32 bits (arrays of more rows would not fit
+    // any device).
+    if (gemk::scan_rows(s->tokens, s->channels) >= int64_t{1} << 27) return GEM_EINVAL;
     if (s->tokens > 0 && (!s->x || !s->gate)) return GEM_EINVAL;
     if (!aligned(s->x, element(s->dtype)) || !aligned(s->gate, element(s->dtype)) ||
         !aligned(s->offsets, 8) || !aligned(s->h0, 4))
@@ -104,8 +102,8 @@ int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out)
     const int rc = [&]() -> int {
         OPS_HIP(hipGetDevice(&o->device));
         OPS_HIP(hipDeviceGetAttribute(&o->dev.cus, hipDeviceAttributeMultiprocessorCount, o->device));
-        if (scratch_bytes > INT64_MAX - kFixed) return GEM_ENOMEM;
-        const size_t bytes = static_cast<size_t>(scratch_bytes + kFixed);
+        if (scratch_bytes > INT64_MAX - gemk::kFixedScratch) return GEM_ENOMEM;
+        const size_t bytes = static_cast<size_t>(scratch_bytes + gemk::kFixedScratch);
         const hipError_t e = hipMalloc(&o->memory, bytes);
         if (e != hipSuccess) {
             gemk::note_hip_error("gem_ops.cpp", "hipMalloc", e, __LINE__);
@@ -114,12 +112,9 @@ int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out)
             return GEM_ENOMEM;
         }
         char* base = static_cast<char*>(o->memory);
-        o->dev.counters = base;
-        o->dev.scratch = base + kCounterBytes;
-        o->dev.scan = base + kFixed;
+        o->dev.scratch = base;
+        o->dev.scan = base + gemk::kFixedScratch;
         o->dev.scan_bytes = scratch_bytes;
-        OPS_HIP(hipMemsetAsync(o->memory, 0, bytes, o->stream));
-        OPS_HIP(hipStreamSynchronize(o->stream));
         return GEM_OK;
     }();
     if (rc != GEM_OK) {
@@ -211,7 +206,7 @@ int gem_scan_scratch(int64_t tokens, int32_t channels, int64_t* bytes)
 int gem_scan_state_rows(int64_t tokens, int64_t* rows)
 {
     if (!rows || tokens < 0 || tokens > kTokensMax) return GEM_EINVAL;
-    *rows = (tokens + gemk::kScanTile - 1) / gemk::kScanTile;
+    *rows = (tokens + gemk::kStateTokens - 1) / gemk::kStateTokens;
     return GEM_OK;
 }
 

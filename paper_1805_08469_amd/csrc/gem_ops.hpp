@@ -16,7 +16,7 @@ void note_hip_error(const char* file, const char* what, hipError_t e, int line);
 constexpr int64_t kFixedScratch = int64_t{8} << 20;
 
 // Tokens between two kept states of a recurrence.
-constexpr int kScanTile = 128;
+constexpr int kStateTokens = 8;
 
 // Rows of logits, and what a launch over them needs.
 struct LogitArgs {
@@ -72,15 +72,14 @@ struct ScanBackArgs {
 // What a handle gives a launch.
 struct OpsDevice {
     int32_t cus;             // compute units
-    void* counters;          // 256 bytes, zero when the handle is made
     void* scratch;           // kFixedScratch bytes
-    void* scan;              // scan_bytes bytes, zero when the handle is made
+    void* scan;              // scan_bytes bytes
     int64_t scan_bytes;
 };
 
 hipError_t launch_scores(const ScoreArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_distill(const DistillArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
-int64_t scan_tiles(int64_t tokens, int64_t channels);
+int64_t scan_rows(int64_t tokens, int64_t channels);
 int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);
 hipError_t launch_scan_forward(const ScanArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_scan_backward(const ScanBackArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);

@@ -17,8 +17,8 @@ namespace gemk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr int kUnroll = 4;                 // vectors of a thread in flight, twice
+constexpr int kMostWaves = 16;             // of a block
 
 // ---- running sums of exponentials -----------------------------------------------
 
@@ -55,6 +55,7 @@ struct Reference {
 struct Run {
     Reference at;
     float limit = -kInf;       // a logit above it moves the reference
+    bool wide = false;         // some thread of the wave has a wide one
     float s = 0.0f, t = 0.0f;
 };
 
@@ -69,31 +70,37 @@ __device__ __forceinline__ void shift_sums(float& s, float& t, float d)
     s *= c;
 }
 
+// Moves the reference where `most` is over the limit: seldom, so the wave's threads are asked
+// together.
 template <bool SUM_D>
-__device__ __forceinline__ void rebase(Run& r, float ref, float scale, float reach)
+__device__ __forceinline__ void rebase(Run& r, float most, float scale, float reach)
 {
-    const Reference from = r.at;
-    r.at.set(ref, scale);
-    r.limit = ref + reach;
-    if (from.ref > -kInf)      // else nothing is summed but zeros and NaN
-        shift_sums<SUM_D>(r.s, r.t, (from.ref - ref) * scale + (r.at.skew(scale) - from.skew(scale)));
+    if (__builtin_expect(__ballot(most > r.limit) == 0, 1)) return;
+    if (most > r.limit) {
+        const Reference from = r.at;
+        r.at.set(most, scale);
+        r.limit = most + reach;
+        if (from.ref > -kInf)  // else nothing is summed but zeros and NaN
+            shift_sums<SUM_D>(r.s, r.t, (from.ref - most) * scale + (r.at.skew(scale) - from.skew(scale)));
+    }
+    r.wide = __ballot(r.at.wide) != 0;
 }
 
 template <bool SUM_D, int N>
 __device__ __forceinline__ void add(Run& r, const float (&x)[N], float most, float scale, float reach)
 {
-    if (most > r.limit) rebase<SUM_D>(r, most, scale, reach);
+    rebase<SUM_D>(r, most, scale, reach);
     const auto sum = [&](float d) {
         const float e = __builtin_amdgcn_exp2f(d);
         r.s += e;
         if constexpr (SUM_D) r.t = __builtin_fmaf(e, __builtin_fmaxf(d, kLeast), r.t);
     };
-    if (!r.at.wide) {
+    if (__builtin_expect(!r.wide, 1)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) sum(__builtin_fmaf(x[i], scale, -r.at.rc));
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum((x[i] - r.at.ref) * scale);
+        for (int i = 0; i < N; ++i) sum(r.at.exponent(x[i], scale));
     }
 }
 
@@ -103,7 +110,7 @@ struct Sums {
     float ref, s, t;
 };
 
-template <bool SUM_D>
+template <int WAVES, bool SUM_D>
 __device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*lds)[4])
 {
     const float top = wave_max(r.at.ref);
@@ -120,9 +127,9 @@ __device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*ld
     __syncthreads();
     Sums out{lds[0][0], 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) out.ref = __builtin_fmaxf(out.ref, lds[w][0]);
+    for (int w = 1; w < WAVES; ++w) out.ref = __builtin_fmaxf(out.ref, lds[w][0]);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         s = lds[w][1];
         t = lds[w][2];
         if (lds[w][0] > -kInf) shift_sums<SUM_D>(s, t, (lds[w][0] - out.ref) * scale);
@@ -133,7 +140,7 @@ __device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*ld
     return out;
 }
 
-__device__ __forceinline__ float block_sum(float v, float* lds)
+template <int WAVES> __device__ __forceinline__ float block_sum(float v, float* lds)
 {
     v = wave_sum(v);
     __syncthreads();
@@ -141,11 +148,11 @@ __device__ __forceinline__ float block_sum(float v, float* lds)
     __syncthreads();
     v = lds[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) v += lds[w];
+    for (int w = 1; w < WAVES; ++w) v += lds[w];
     return v;
 }
 
-__device__ __forceinline__ float block_max(float v, float* lds)
+template <int WAVES> __device__ __forceinline__ float block_max(float v, float* lds)
 {
     v = wave_max(v);
     __syncthreads();
@@ -153,7 +160,7 @@ __device__ __forceinline__ float block_max(float v, float* lds)
     __syncthreads();
     v = lds[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) v = __builtin_fmaxf(v, lds[w]);
+    for (int w = 1; w < WAVES; ++w) v = __builtin_fmaxf(v, lds[w]);
     return v;
 }
 
@@ -187,44 +194,63 @@ template <class T> struct Part {
     }
 };
 
-template <int N> __device__ __forceinline__ float most_of(const float (&x)[N])
+// The largest that is a number.  (Written out: for a maximum of bits that might be a
+// signalling NaN the compiler quiets them first.)
+__device__ __forceinline__ float max3(float a, float b, float c)
 {
-    float m = __builtin_fmaxf(x[0], x[1]);
-#pragma unroll
-    for (int i = 2; i < N; i += 2) m = __builtin_fmaxf(__builtin_fmaxf(m, x[i]), x[i + 1]);
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
     return m;
 }
+template <int N> __device__ __forceinline__ float most_of(const float (&x)[N])
+{
+    float m = max3(x[0], x[1], x[2]);
+#pragma unroll
+    for (int i = 3; i + 1 < N; i += 2) m = max3(m, x[i], x[i + 1]);
+    return max3(m, x[N - 1], x[N - 1]);
+}
 
-// f(v, vector, inside) for each vector v of the part, kUnroll loads ahead.  inside is
-// false past the end, where the last vector is given again.
-template <class F>
+// The bits of two -inf, or of one.
+template <class T> __device__ __forceinline__ uint32_t lowest() { return sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u; }
+
+// Non-temporal: a row's bytes are read once, or again when the caches have long passed them.
+__device__ __forceinline__ u32x4 read_once(const u32x4* p) { return __builtin_nontemporal_load(p); }
+
+// f(v, vector) for each vector v of the part by its thread, UNROLL loads ahead.  Every
+// thread calls it equally often (f may ask the wave); inside is false past the end, where
+// the last vector is given again.
+template <int THREADS, int UNROLL, class F>
 __device__ __forceinline__ void stream(const u32x4* body, int nvec, F f)
 {
     if (nvec == 0) return;
+    constexpr int kRound = THREADS * UNROLL;
     const int tid = threadIdx.x, last = nvec - 1;
-    u32x4 next[kUnroll];
+    u32x4 next[UNROLL];
+    const auto load = [&](int base) {
+        if (base + kRound <= nvec) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int v = tid + u * kThreads;
-        next[u] = body[v < last ? v : last];
-    }
-    for (int base = 0; base < nvec; base += kThreads * kUnroll) {
-        u32x4 cur[kUnroll];
+            for (int u = 0; u < UNROLL; ++u) next[u] = read_once(body + base + tid + u * THREADS);
+        } else {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) cur[u] = next[u];
-        if (base + kThreads * kUnroll < nvec) {
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int v = base + tid + (kUnroll + u) * kThreads;
-                next[u] = body[v < last ? v : last];
+            for (int u = 0; u < UNROLL; ++u) {
+                const int v = base + tid + u * THREADS;
+                if (base + u * THREADS < nvec) next[u] = read_once(body + (v < last ? v : last));
             }
         }
+    };
+    load(0);
+    int base = 0;
+    for (; base + kRound <= nvec; base += kRound) {
+        u32x4 cur[UNROLL];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int v = base + tid + u * kThreads;
-            f(v, cur[u], v < nvec);
-        }
+        for (int u = 0; u < UNROLL; ++u) cur[u] = next[u];
+        load(base + kRound);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) f(base + tid + u * THREADS, cur[u], true);
     }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+        if (base + u * THREADS < nvec) f(base + tid + u * THREADS, next[u], base + tid + u * THREADS < nvec);
 }
 
 // ---- alternatives ----------------------------------------------------------------
@@ -251,16 +277,21 @@ __device__ __forceinline__ int key_token(uint64_t key) { return static_cast<int>
 // The k largest of a row lie in the k groups of eight whose largest elements rank
 // highest (each group ahead of another has an element that ranks ahead of all of the
 // other's).  So the pass over the row keeps one key a group in LDS, and only k groups
-// are looked at again.  bfloat16 logits need 16 bits of a key.
+// are looked at again.  The key of a group is its largest element as it is; of bfloat16 logits
+// 16 bits.
 constexpr int kGroup = 8;
 template <class T> struct GroupKey;
 template <> struct GroupKey<uint16_t> {
     using Type = uint16_t;
-    static constexpr int kShift = 16;      // key = order >> kShift
+    static constexpr int kShift = 16;      // bits of an order that a key does not need
+    static __device__ Type of(float v) { return static_cast<uint16_t>(__float_as_uint(v) >> 16); }
+    static __device__ uint32_t order_of(Type k) { return order(__uint_as_float(static_cast<uint32_t>(k) << 16)) >> 16; }
 };
 template <> struct GroupKey<float> {
-    using Type = uint32_t;
+    using Type = float;
     static constexpr int kShift = 0;
+    static __device__ Type of(float v) { return v; }
+    static __device__ uint32_t order_of(Type k) { return order(k); }
 };
 // Elements of a part: 32 KiB of group keys.
 template <class T> constexpr int kPartMax = (32 << 10) / static_cast<int>(sizeof(typename GroupKey<T>::Type)) * kGroup;
@@ -272,7 +303,7 @@ struct TopLds {
     uint64_t list[kList];
     uint64_t sel[GEM_TOP_MAX];
     uint32_t high[kThreads];
-    int wave[2][kWaves];
+    int wave[2][kThreads / 64];
     int count;
 };
 
@@ -312,7 +343,7 @@ __device__ uint64_t bound_of(TopLds& l, int mine, int k, int fit, F key)
         __syncthreads();
         n = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) n += l.wave[turn][w];
+        for (int w = 0; w < kThreads / 64; ++w) n += l.wave[turn][w];
         turn ^= 1;
         if (n >= k) {
             bound = trial;
@@ -335,16 +366,16 @@ __device__ void select_top(TopLds& l, const Part<T>& part, const typename GroupK
     if (tid == 0) l.count = 0;
     __syncthreads();
     // A first bound: the k-th of the threads' largest elements (16 bits of their keys).
-    uint32_t q[kWaves];
+    uint32_t q[kThreads / 64];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) q[w] = l.high[lane + 64 * w];
+    for (int w = 0; w < kThreads / 64; ++w) q[w] = l.high[lane + 64 * w];
     uint32_t low = 0;
 #pragma unroll 1
     for (int bit = 31 - shift; bit >= 16 - shift; --bit) {
         const uint32_t trial = low | (1u << bit);
         int n = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) n += __builtin_popcountll(__ballot(q[w] >= trial));
+        for (int w = 0; w < kThreads / 64; ++w) n += __builtin_popcountll(__ballot(q[w] >= trial));
         if (n >= k) low = trial;
     }
     if (low == 0) low = 1;
@@ -353,12 +384,12 @@ __device__ void select_top(TopLds& l, const Part<T>& part, const typename GroupK
     constexpr int kLanes = kGroup / kVec<T>;
     if (seen >= low && tid % kLanes == 0)
         for (int g = 1 + tid / kLanes; g < groups - 1; g += kThreads / kLanes) {
-            const uint32_t o = keys[g];
+            const uint32_t o = GroupKey<T>::order_of(keys[g]);
             if (o >= low) push(l, (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~g));
         }
     if (tid < 2) {
         const int g = tid == 0 ? 0 : groups - 1;
-        const uint32_t o = keys[g];
+        const uint32_t o = GroupKey<T>::order_of(keys[g]);
         if (o >= low) push(l, (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~g));
     }
     __syncthreads();
@@ -367,7 +398,7 @@ __device__ void select_top(TopLds& l, const Part<T>& part, const typename GroupK
         // Many equal groups: a bound that leaves few enough.
         const auto key = [&](int j) {
             const int g = tid + j * kThreads;
-            const uint32_t o = keys[g];
+            const uint32_t o = GroupKey<T>::order_of(keys[g]);
             return o ? (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~g) : uint64_t{0};
         };
         const int mine = tid < groups ? (groups - tid + kThreads - 1) / kThreads : 0;
@@ -450,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a, int6
     constexpr int shift = GroupKey<T>::kShift;
     extern __shared__ uint32_t dynamic_lds[];
     Key* keys = reinterpret_cast<Key*>(dynamic_lds);
-    __shared__ float lds[kWaves][4];
+    __shared__ float lds[kThreads / 64][4];
     __shared__ TopLds top;
     const int64_t r = row0 + blockIdx.x / parts;
     const int q = blockIdx.x % parts, tid = threadIdx.x;
@@ -459,7 +490,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a, int6
     const float scale = a.l.scale, reach = 20.0f / scale;
     const int groups = (part.nvec * kVec<T> + kGroup - 1) / kGroup + 2;
     Run run;
-    uint32_t high = 0, seen = 0;   // largest key of the thread's elements, and of its groups
+    float high = -kInf, seen = -kInf;  // the largest of the thread's elements, and of its groups
     if (tid < 64) {
         float x[kVec<T>];
         part.edge(x);
@@ -467,32 +498,31 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a, int6
         add<true>(run, x, m, scale, reach);
         if constexpr (TOP)
             if (tid < 2) {
-                high = seen = order(m) >> shift;
-                keys[tid == 0 ? 0 : groups - 1] = static_cast<Key>(high);
+                high = seen = __builtin_fmaxf(high, m);
+                keys[tid == 0 ? 0 : groups - 1] = GroupKey<T>::of(m);
             }
     }
-    stream(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
+    stream<kThreads, kUnroll>(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
         float x[kVec<T>];
-        unpack(raw, x);
-        float m = most_of(x);
+        unpack(inside ? raw : u32x4{lowest<T>(), lowest<T>(), lowest<T>(), lowest<T>()}, x);
+        const float m = most_of(x);
+        add<true>(run, x, m, scale, reach);
         if constexpr (TOP) {
-            float both = inside ? m : -kInf;
-            if constexpr (kVec<T> < kGroup) both = __builtin_fmaxf(both, __shfl_xor(both, 1));
-            const uint32_t o = order(both) >> shift;
-            seen = o > seen ? o : seen;
+            high = max3(high, m, m);
             if constexpr (kVec<T> < kGroup) {
-                const uint32_t own = inside ? order(m) >> shift : 0;
-                high = own > high ? own : high;
-                if (inside && (v & 1) == 0) keys[1 + v / 2] = static_cast<Key>(o);
-            } else {
-                high = seen;
-                if (inside) keys[1 + v] = static_cast<Key>(o);
+                // Two neighbours share a group.
+                const float other = __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(m), 0xB1, 0xF, 0xF, true));
+                const float both = max3(m, other, other);
+                seen = max3(seen, both, both);
+                if (inside && (v & 1) == 0) keys[1 + v / 2] = GroupKey<T>::of(both);
+            } else if (inside) {
+                keys[1 + v] = GroupKey<T>::of(m);
             }
         }
-        if (inside) add<true>(run, x, m, scale, reach);
     });
-    const Sums u = block_sums<true>(run, scale, lds);
-    if constexpr (TOP) select_top(top, part, keys, groups, high, seen, a.top_k);
+    const Sums u = block_sums<kThreads / 64, true>(run, scale, lds);
+    if constexpr (TOP)
+        select_top(top, part, keys, groups, order(high) >> shift, order(kVec<T> < kGroup ? seen : high) >> shift, a.top_k);
     if (parts == 1) {
         write_scores(a, r, row, u, top.sel);
     } else {
@@ -511,7 +541,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const ScoreArgs a, int64
 {
     extern __shared__ uint32_t dynamic_lds[];
     uint64_t* keys = reinterpret_cast<uint64_t*>(dynamic_lds);
-    __shared__ float lds[kWaves][4];
+    __shared__ float lds[kThreads / 64][4];
     __shared__ TopLds top;
     const int64_t r = row0 + blockIdx.x;
     const int tid = threadIdx.x;
@@ -527,7 +557,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const ScoreArgs a, int64
     const int n = parts * a.top_k;
     for (int j = tid; j < n; j += kThreads) keys[j] = tops[static_cast<int64_t>(blockIdx.x) * n + j];
     if (tid == 0) top.count = 0;
-    const Sums u = block_sums<true>(run, a.l.scale, lds);
+    const Sums u = block_sums<kThreads / 64, true>(run, a.l.scale, lds);
     if (a.top_k) {
         const int mine = tid < n ? (n - tid + kThreads - 1) / kThreads : 0;
         const auto key = [&](int j) { return keys[tid + j * kThreads]; };
@@ -545,176 +575,195 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const ScoreArgs a, int64
 // ---- distillation ----------------------------------------------------------------
 
 struct DistillLds {
-    float sums[kWaves][4];
-    float red[kWaves];
-    int ids[GEM_TOP_MAX];
+    float sums[kMostWaves][4];
+    float red[kMostWaves];
+    alignas(16) int ids[GEM_TOP_MAX];
+    uint32_t edges[2];         // marks of the head and the tail
 };
 
-// Thread i's entry of the row's record: its token (-1: none), log probability and
-// probability, and p_t.
+// Thread i's entry of a row's record as it is given.
+struct Entry {
+    int id = -1;
+    float lp = -kInf;
+};
+
+__device__ __forceinline__ Entry entry_of(const DistillArgs& a, int64_t r)
+{
+    Entry e;
+    const int tid = threadIdx.x;
+    if (tid < a.k) {
+        e.id = a.ids[r * a.k + tid];
+        e.lp = a.lp[r * a.k + tid];
+        if (e.id < 0 || e.id >= a.l.vocab) e.id = -1;
+    }
+    return e;
+}
+
+// Thread i's token, -1 if an earlier entry has it: of equal ones the first counts.
+__device__ __forceinline__ int distinct(const Entry& e, int k, DistillLds& l)
+{
+    const int tid = threadIdx.x;
+    if (tid < GEM_TOP_MAX) l.ids[tid] = e.id;
+    __syncthreads();
+    if (tid >= k) return -1;
+    bool again = false;
+    for (int i = 0; i < tid; i += 16) {
+        int4 ids[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ids[j] = reinterpret_cast<const int4*>(l.ids + i)[j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = tid - i - 4 * j;
+            again |= (ids[j].x == e.id && at > 0) || (ids[j].y == e.id && at > 1) || (ids[j].z == e.id && at > 2) ||
+                     (ids[j].w == e.id && at > 3);
+        }
+    }
+    return again ? -1 : e.id;
+}
+
+// Thread i's entry as it counts: its token (-1: none), log probability and probability, and
+// p_t; and the token's logit.
 struct Teacher {
     int id = -1;
-    float lp = 0.0f, p = 0.0f, pt = 0.0f;
+    float lp = 0.0f, p = 0.0f, pt = 0.0f, x = -kInf;
 };
 
-__device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, int64_t r, DistillLds& l)
+template <int WAVES>
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const Entry& e, DistillLds& l)
 {
     Teacher t;
-    const int tid = threadIdx.x;
-    float lp = -kInf;
-    if (tid < a.k) {
-        t.id = a.ids[r * a.k + tid];
-        lp = a.lp[r * a.k + tid];
-        if (t.id < 0 || t.id >= a.l.vocab) t.id = -1;
-        l.ids[tid] = t.id;
-    }
-    __syncthreads();
-    if (tid < a.k)
-        for (int i = 0; i < tid; ++i)
-            if (l.ids[i] == t.id) t.id = -1;
-    if (t.id < 0) lp = -kInf;
+    t.id = distinct(e, a.k, l);
+    const float lp = t.id < 0 ? -kInf : e.lp;
     if (a.tail) {
         t.lp = lp;
         t.p = t.id >= 0 ? expf(lp) : 0.0f;
-        t.pt = __builtin_fmaxf(0.0f, 1.0f - block_sum(t.p, l.red));
+        t.pt = __builtin_fmaxf(0.0f, 1.0f - block_sum<WAVES>(t.p, l.red));
     } else {
-        const float top = block_max(lp, l.red);
+        const float top = block_max<WAVES>(lp, l.red);
         t.p = t.id >= 0 && top > -kInf ? expf(lp - top) : 0.0f;
-        const float sum = block_sum(t.p, l.red);
+        const float sum = block_sum<WAVES>(t.p, l.red);
         t.lp = lp - (top + logf(sum));
         t.p = sum > 0.0f ? t.p / sum : 0.0f;
     }
     return t;
 }
 
-// Marks of the part's listed tokens: a bit for each element of each vector, a vector's
-// bits where its thread finds those of its kUnroll vectors in one word.
-__device__ __forceinline__ int mark_byte(int v)
+// Marks a listed token of the part: a bit for its element in the byte of its vector v,
+// byte_of(v), or in that of the head or the tail.
+template <class T, class F>
+__device__ __forceinline__ void mark(const Part<T>& part, uint32_t* marks, DistillLds& l, int id, F byte_of)
 {
-    constexpr int kRound = kThreads * kUnroll;
-    return v / kRound * kRound + v % kThreads * kUnroll + v % kRound / kThreads;
-}
-
-template <class T>
-__device__ __forceinline__ void mark(const Part<T>& part, uint8_t* marks, uint32_t* edges, int id)
-{
-    const int at = id - part.begin;
+    const int at = id - part.begin, end = part.head + part.nvec * kVec<T>;
     if (id < 0 || at < 0 || at >= part.n) return;
-    const int end = part.head + part.nvec * kVec<T>;
     if (at < part.head) {
-        atomicOr(&edges[0], 1u << at);
+        atomicOr(&l.edges[0], 1u << at);
     } else if (at >= end) {
-        atomicOr(&edges[1], 1u << (at - end));
+        atomicOr(&l.edges[1], 1u << (at - end));
     } else {
-        const int v = (at - part.head) / kVec<T>, byte = mark_byte(v);
-        atomicOr(reinterpret_cast<uint32_t*>(marks) + byte / 4,
-                 1u << (byte % 4 * 8 + (at - part.head) % kVec<T>));
+        const int byte = byte_of((at - part.head) / kVec<T>);
+        atomicOr(&marks[byte / 4], 1u << (byte % 4 * 8 + (at - part.head) % kVec<T>));
     }
 }
+__host__ __device__ constexpr int mark_words(int nvec) { return (nvec + 3) / 4; }
 
-__host__ __device__ constexpr int mark_words(int nvec)
+// Without the listed elements.
+template <int N> __device__ __forceinline__ void drop(float (&x)[N], uint32_t listed)
 {
-    return (nvec + kThreads * kUnroll - 1) / (kThreads * kUnroll) * kThreads;
-}
-
-// The part's sums over unlisted tokens (s) and listed ones (t).  Without marks every
-// token counts as unlisted.
-template <class T, bool MARKS>
-__device__ __forceinline__ Sums distill_sums(const DistillArgs& a, const Part<T>& part, const uint32_t* marks,
-                                             const uint32_t* edges, DistillLds& l)
-{
-    const float scale = a.l.scale, reach = 20.0f / scale;
-    Run run;
-    const auto take = [&](float (&x)[kVec<T>], uint32_t listed) {
-        const float m = most_of(x);
-        if (MARKS && listed) {
-            if (m > run.limit) rebase<false>(run, m, scale, reach);
+    if (__builtin_expect(__ballot(listed != 0) == 0, 0)) return;
 #pragma unroll
-            for (int i = 0; i < kVec<T>; ++i) {
-                const float e = __builtin_amdgcn_exp2f(run.at.exponent(x[i], scale));
-                if (listed >> i & 1u) run.t += e;
-                else run.s += e;
-            }
-        } else {
-            add<false>(run, x, m, scale, reach);
-        }
-    };
-    if (threadIdx.x < 64) {
-        float x[kVec<T>];
-        part.edge(x);
-        take(x, MARKS && threadIdx.x < 2 ? edges[threadIdx.x] : 0u);
-    }
-    stream(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
-        if (!inside) return;
-        float x[kVec<T>];
-        unpack(raw, x);
-        uint32_t listed = 0;
-        if constexpr (MARKS) listed = reinterpret_cast<const uint8_t*>(marks)[mark_byte(v)];
-        take(x, listed);
-    });
-    return block_sums<false>(run, scale, l.sums);
+    for (int i = 0; i < N; ++i) x[i] = listed >> i & 1u ? -kInf : x[i];
 }
 
-// The row's loss, from thread i's entry and its logit.
-__device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t, float x, const Sums& u, DistillLds& l)
+// The head and the tail, without their marked elements.
+template <class T>
+__device__ __forceinline__ void take_edges(const Part<T>& part, Run& run, const DistillLds& l, float scale, float reach)
+{
+    if (threadIdx.x >= 64) return;
+    float x[kVec<T>];
+    part.edge(x);
+    drop(x, threadIdx.x < 2 ? l.edges[threadIdx.x] : 0u);
+    add<false>(run, x, most_of(x), scale, reach);
+}
+
+// Listed tokens' exponentials are summed apart, in t, by their entries' threads.
+template <class T>
+__device__ __forceinline__ void take_listed(const Part<T>& part, Run& run, const Teacher& t, float scale, float reach)
+{
+    const float x = t.id >= part.begin && t.id < part.begin + part.n ? t.x : -kInf;
+    rebase<false>(run, x, scale, reach);
+    run.t += __builtin_amdgcn_exp2f(run.at.exponent(x, scale));
+}
+
+// The row's loss, from thread i's entry.
+template <int WAVES>
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t, const Sums& u, DistillLds& l)
 {
     const float all = u.s + u.t, ls = __builtin_log2f(all);
     float part = 0.0f;
-    if (t.p > 0.0f) part = t.p * (t.lp - log_prob(a.l, x, u.ref, ls));
-    float loss = block_sum(part, l.red);
+    if (t.p > 0.0f) part = t.p * (t.lp - log_prob(a.l, t.x, u.ref, ls));
+    float loss = block_sum<WAVES>(part, l.red);
     if (t.pt > 0.0f)
         loss += u.s == 0.0f ? kInf : t.pt * (logf(t.pt) - (__builtin_log2f(u.s) - ls) * kLn2);
     return loss;
 }
 
-// The part's gradient: every token by the unlisted tokens' form, then the listed.
-template <class T>
-__device__ __forceinline__ void write_grad(const DistillArgs& a, const Part<T>& part, T* grad, const Teacher& t, float x,
-                                           const Sums& u, float w)
-{
-    const float scale = a.l.scale, f = w * a.l.inv_t;
-    const float all = u.s + u.t;
-    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-    const float rest = t.pt > 0.0f && u.s != 0.0f ? t.pt / u.s : 0.0f;
+// A row's gradient: c 2^d of unlisted tokens, and of a listed one f (2^d inv - p).  Every
+// element is stored as an unlisted token's, and the listed ones again when those stores are
+// done (stores_done), which spares the vectors a look at the marks.
+struct Grad {
     Reference at;
-    at.set(u.ref, scale);
-    const float c = f * (inv - rest) * __builtin_amdgcn_exp2f(-at.skew(scale));
-    T* out = grad + part.begin;
-    if (threadIdx.x < 2) {
-        const int from = part.edge_at(), m = part.edge_n();
-        for (int i = from; i < from + m; ++i)
-            store(out, i, c * __builtin_amdgcn_exp2f(at.exponent(load(part.p, i), scale)));
+    float c, f, inv;
+
+    __device__ Grad(const DistillArgs& a, const Teacher& t, const Sums& u, float w)
+    {
+        at.set(u.ref, a.l.scale);
+        f = w * a.l.inv_t;
+        const float all = u.s + u.t;
+        inv = all == 0.0f ? 0.0f : 1.0f / all;
+        const float rest = t.pt > 0.0f && u.s != 0.0f ? t.pt / u.s : 0.0f;
+        c = f * (inv - rest) * __builtin_amdgcn_exp2f(-at.skew(a.l.scale));
     }
-    T* body = out + part.head;
-    // The gradient's own rows may be aligned otherwise than the logits'.
-    const bool whole = (reinterpret_cast<uintptr_t>(body) & 15u) == 0;
-    stream(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
-        if (!inside) return;
+
+    // Vector v of the part; whole: its rows are aligned as the logits'.
+    template <class T>
+    __device__ __forceinline__ void vector(T* body, uint32_t v, u32x4 raw, bool whole, float scale) const
+    {
         float y[kVec<T>];
         unpack(raw, y);
-        if (!at.wide) {
+        if (__builtin_expect(!at.wide, 1)) {
 #pragma unroll
-            for (int i = 0; i < kVec<T>; ++i)
-                y[i] = c * __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], scale, -at.rc));
+            for (int i = 0; i < kVec<T>; ++i) y[i] = c * __builtin_amdgcn_exp2f(__builtin_fmaf(y[i], scale, -at.rc));
         } else {
 #pragma unroll
             for (int i = 0; i < kVec<T>; ++i) y[i] = c * __builtin_amdgcn_exp2f((y[i] - at.ref) * scale);
         }
         if (whole) {
-            __builtin_nontemporal_store(pack(y), reinterpret_cast<u32x4*>(body) + v);
+            __builtin_nontemporal_store(pack(y), reinterpret_cast<u32x4*>(reinterpret_cast<char*>(body) + v * 16u));
         } else {
 #pragma unroll
             for (int i = 0; i < kVec<T>; ++i) store(body, static_cast<int64_t>(v) * kVec<T> + i, y[i]);
         }
-    });
-    // The listed tokens' elements are stored again, behind the others.
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (t.id >= part.begin && t.id < part.begin + part.n)
-        store(grad, t.id, f * (__builtin_amdgcn_exp2f((x - at.ref) * scale) * inv - t.p));
-}
+    }
 
-template <class T>
+    template <class T> __device__ __forceinline__ void edges(const LogitArgs& l, const Part<T>& part, T* grad) const
+    {
+        if (threadIdx.x >= 2) return;
+        T* out = grad + part.begin;
+        const int from = part.edge_at(), m = part.edge_n();
+        for (int i = from; i < from + m; ++i)
+            store(out, i, c * __builtin_amdgcn_exp2f(at.exponent(load(part.p, i), l.scale)));
+    }
+
+    __device__ float listed(const Teacher& t, float scale) const
+    {
+        return f * (__builtin_amdgcn_exp2f((t.x - at.ref) * scale) * inv - t.p);
+    }
+};
+
+// Before a barrier: behind it the block's stores so far are in memory.
+__device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int THREADS, class T>
 __device__ __forceinline__ void no_grad(const Part<T>& part, T* grad)
 {
     T* out = grad + part.begin;
@@ -722,60 +771,81 @@ __device__ __forceinline__ void no_grad(const Part<T>& part, T* grad)
     int head = (kVec<T> - off) & (kVec<T> - 1);
     if (head > part.n) head = part.n;
     const int nvec = (part.n - head) / kVec<T>, end = head + nvec * kVec<T>;
-    for (int i = threadIdx.x; i < head; i += kThreads) store(out, i, 0.0f);
-    for (int i = end + threadIdx.x; i < part.n; i += kThreads) store(out, i, 0.0f);
-    for (int v = threadIdx.x; v < nvec; v += kThreads)
+    for (int i = threadIdx.x; i < head; i += THREADS) store(out, i, 0.0f);
+    for (int i = end + threadIdx.x; i < part.n; i += THREADS) store(out, i, 0.0f);
+    for (int v = threadIdx.x; v < nvec; v += THREADS)
         __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>(out + head) + v);
 }
 
-// What a block does with its part: sums alone (left in part_sums, and the logits of the
-// part's listed tokens in part_x, [rows][k]: the gradient may be written over the logits
+// What a block does with its part of a row: sums alone (left in part_sums, and the logits of
+// the part's listed tokens in part_x, [rows][k]: the gradient may be written over the logits
 // while another part's block needs them), the rest from those, or, with one part a row, both.
 enum : int { kSums = 1, kRest = 2 };
+
+// The part's sums over unlisted tokens (s); without MARKS over all.
+template <class T, bool MARKS>
+__device__ __forceinline__ void take_part(const Part<T>& part, Run& run, const uint32_t* marks, const DistillLds& l,
+                                          float scale, float reach)
+{
+    take_edges(part, run, l, scale, reach);
+    stream<kThreads, kUnroll>(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
+        float x[kVec<T>];
+        unpack(inside ? raw : u32x4{lowest<T>(), lowest<T>(), lowest<T>(), lowest<T>()}, x);
+        if constexpr (MARKS) drop(x, inside ? reinterpret_cast<const uint8_t*>(marks)[v] : 0u);
+        add<false>(run, x, most_of(x), scale, reach);
+    });
+}
 
 template <class T, int STEP>
 __global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a, int64_t row0, int parts, int len,
                                                            PartSums* part_sums, float* part_x)
 {
-    extern __shared__ uint32_t dynamic_lds[];
+    constexpr int WAVES = kThreads / 64;
+    extern __shared__ uint32_t marks[];
     __shared__ DistillLds l;
-    __shared__ uint32_t edges[2];
     const int blocks = STEP == kRest && !a.grad ? 1 : parts;       // of a row
     const int64_t i = blockIdx.x / blocks, r = row0 + i;
     const int q = blockIdx.x % blocks, tid = threadIdx.x;
     const T* row = static_cast<const T*>(a.l.z) + r * a.l.stride;
     T* grad = a.grad ? static_cast<T*>(a.grad) + r * a.grad_stride : nullptr;
     const Part<T> part(row, a.l.vocab, q * len, len);
-    const float w = a.weight ? a.weight[r] : 1.0f;
+    const float w = a.weight ? a.weight[r] : 1.0f, scale = a.l.scale;
     if (w == 0.0f) {
         if (STEP & kRest) {
             if (tid == 0 && q == 0 && a.loss) a.loss[r] = 0.0f;
-            if (grad) no_grad(part, grad);
+            if (grad) no_grad<kThreads>(part, grad);
         }
         return;
     }
-    const Teacher t = teacher_of(a, r, l);
+    const Entry e = entry_of(a, r);
+    if (STEP & kSums) {
+        if (a.tail)
+            for (int j = tid; j < mark_words(part.nvec); j += kThreads) marks[j] = 0;
+        if (tid < 2) l.edges[tid] = 0;
+    }
+    Teacher t;
+    if constexpr (STEP & kRest) t = teacher_of<WAVES>(a, e, l);
+    else t.id = a.tail ? distinct(e, a.k, l) : e.id;
+    if (t.id >= 0) t.x = STEP & kSums ? load(row, t.id) : part_x[i * a.k + tid];
     Sums u{0.0f, 0.0f, 0.0f};
+    Run run;
     if constexpr (STEP & kSums) {
+        const float reach = 20.0f / scale;
         if (a.tail) {
-            const int words = mark_words(part.nvec);
-            for (int i = tid; i < words; i += kThreads) dynamic_lds[i] = 0;
-            if (tid < 2) edges[tid] = 0;
+            mark(part, marks, l, t.id, [](int v) { return v; });
             __syncthreads();
-            mark(part, reinterpret_cast<uint8_t*>(dynamic_lds), edges, t.id);
-            __syncthreads();
-            u = distill_sums<T, true>(a, part, dynamic_lds, edges, l);
+            take_part<T, true>(part, run, marks, l, scale, reach);
+            take_listed(part, run, t, scale, reach);
         } else {
-            u = distill_sums<T, false>(a, part, dynamic_lds, edges, l);
+            take_part<T, false>(part, run, marks, l, scale, reach);
         }
+        u = block_sums<WAVES, false>(run, scale, l.sums);
         if constexpr (!(STEP & kRest)) {
             if (tid == 0) part_sums[blockIdx.x] = PartSums{u.s + u.t == 0.0f ? -kInf : u.ref, u.s, u.t, 0.0f};
-            if (t.id >= part.begin && t.id < part.begin + part.n)
-                part_x[i * a.k + tid] = load(row, t.id);
+            if (t.id >= part.begin && t.id < part.begin + part.n) part_x[i * a.k + tid] = t.x;
             return;
         }
     } else {
-        Run run;
         if (tid < parts) {
             const PartSums p = part_sums[i * parts + tid];
             run.at.ref = p.ref;    // its sums have no skew
@@ -783,19 +853,187 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a, 
             run.s = p.s;
             run.t = p.t;
         }
-        u = block_sums<false>(run, a.l.scale, l.sums);
+        u = block_sums<WAVES, false>(run, scale, l.sums);
     }
-    float x = 0.0f;            // thread i's entry's logit
-    if (t.id >= 0)
-        x = STEP & kSums ? load(row, t.id) : part_x[i * a.k + tid];
-    if (a.loss && q == 0) {
-        const float loss = loss_of(a, t, x, u, l);
-        if (tid == 0) a.loss[r] = loss;
+    const float loss = loss_of<WAVES>(a, t, u, l);     // and every entry's logit is read
+    if (a.loss && q == 0 && tid == 0) a.loss[r] = loss;
+    if (!grad) return;
+    const Grad g(a, t, u, w);
+    T* body = grad + part.begin + part.head;
+    const bool whole = (reinterpret_cast<uintptr_t>(body) & 15u) == 0;
+    g.edges(a.l, part, grad);
+    stream<kThreads, kUnroll>(part.body(), part.nvec, [&](int v, u32x4 raw, bool inside) {
+        if (inside) g.vector(body, v, raw, whole, scale);
+    });
+    stores_done();
+    __syncthreads();
+    if (t.id >= part.begin && t.id < part.begin + part.n) store(grad, t.id, g.listed(t, scale));
+}
+
+// Loss and gradient with a row's vectors in registers, NV of a thread: what they hold is read
+// once (with REST a row has more, which is read twice).  A block goes through rows; as each
+// vector of a gradient is stored the next row's takes its place, so that loads and stores go
+// on through the sums, and a row's listed elements are stored behind the next row's.
+constexpr int kRestUnroll = 2;
+
+template <class T, int THREADS, int NV, bool REST>
+__global__ __launch_bounds__(THREADS, 4) void resident_kernel(const DistillArgs a)
+{
+    constexpr int WAVES = THREADS / 64, kKept = THREADS * NV;
+    extern __shared__ __align__(16) uint32_t marks[];      // a thread's NV bytes, and one of every further vector
+    __shared__ DistillLds l;
+    const uint32_t tid = threadIdx.x;
+    const float scale = a.l.scale, reach = 20.0f / scale;
+    const auto part_of = [&](int64_t r) {
+        return Part<T>(static_cast<const T*>(a.l.z) + r * a.l.stride, a.l.vocab, 0, a.l.vocab);
+    };
+    const auto grad_of = [&](int64_t r) { return static_cast<T*>(a.grad) + r * a.grad_stride; };
+    const auto byte_of = [](int v) { return !REST || v < kKept ? v % THREADS * NV + v / THREADS : v; };
+    float w = 0.0f;
+    // The block's next row from r on that has a weight (or beyond the last), which it sets w to;
+    // the gradients of those before it are zero.
+    const auto next_row = [&](int64_t r) {
+        for (; r < a.l.rows; r += gridDim.x) {
+            w = a.weight ? a.weight[r] : 1.0f;
+            if (w != 0.0f) break;
+            if (tid == 0 && a.loss) a.loss[r] = 0.0f;
+            no_grad<THREADS>(part_of(r), grad_of(r));
+        }
+        return r;
+    };
+    u32x4 d[NV];
+    // The thread's place among a vector's, as something new: places of all vectors, the same
+    // for every row, would be kept in registers.
+    const auto place = [&]() {
+        uint32_t at = tid;
+        asm volatile("" : "+v"(at));
+        return at;
+    };
+    // A vector's bits, as something new: else its elements are kept from one pass to the next.
+    const auto vector = [&](int u) {
+        asm volatile("" : "+v"(d[u]));
+        return d[u];
+    };
+    const auto fetch = [&](const Part<T>& part, int u, uint32_t at) {
+        const uint32_t v = u * THREADS + at, last = part.nvec - 1;
+        d[u] = read_once(reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(part.body()) + (v < last ? v : last) * 16u));
+    };
+    int64_t r = next_row(blockIdx.x);
+    if (r >= a.l.rows) return;
+    for (uint32_t i = tid; i < static_cast<uint32_t>(mark_words(kKept)); i += THREADS) marks[i] = 0;
+    if constexpr (REST)
+        for (int i = kKept / 4 + tid; i < mark_words(a.l.vocab / kVec<T>); i += THREADS) marks[i] = 0;
+    if (tid < 2) l.edges[tid] = 0;
+    Entry e = entry_of(a, r);
+    {
+        const Part<T> part = part_of(r);
+#pragma unroll
+        for (int u = 0; u < NV; ++u)
+            if (u * THREADS < part.nvec) fetch(part, u, tid);
     }
-    if (grad) {
-        __syncthreads();       // every logit of an entry is read before the part is written over
-        write_grad(a, part, grad, t, x, u, w);
+    __syncthreads();
+    int listed_id = -1;        // of the row before
+    float listed_value = 0.0f;
+    T* listed_grad = nullptr;
+    for (;;) {
+        const Part<T> part = part_of(r);
+        T* grad = grad_of(r);
+        if (a.tail) mark(part, marks, l, e.id, byte_of);
+        Teacher t = teacher_of<WAVES>(a, e, l);
+        if (t.id >= 0) t.x = load(part.p, t.id);
+        // Sums, about the largest of the thread's vectors.
+        float most = -kInf;
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            if (u * THREADS < part.nvec) {
+                if ((u + 1) * THREADS > part.nvec) {
+                    const bool inside = static_cast<int>(u * THREADS + place()) < part.nvec;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[u][i] = inside ? d[u][i] : lowest<T>();
+                }
+                float x[kVec<T>];
+                unpack(vector(u), x);
+                most = max3(most, most_of(x), most);
+            }
+            __builtin_amdgcn_sched_barrier(0);         // one vector's elements at a time in registers
+        }
+        Run run;
+        rebase<false>(run, most, scale, reach);
+        uint32_t words[NV / 4] = {};
+        if (a.tail) {
+#pragma unroll
+            for (int i = 0; i < NV / 4; ++i) {
+                words[i] = marks[tid * (NV / 4) + i];
+                marks[tid * (NV / 4) + i] = 0;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            if (u * THREADS < part.nvec) {
+                float x[kVec<T>];
+                unpack(vector(u), x);
+                drop(x, words[u / 4] >> u % 4 * 8 & 0xFFu);
+                if (__builtin_expect(!run.wide, 1)) {
+#pragma unroll
+                    for (int i = 0; i < kVec<T>; ++i) run.s += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -run.at.rc));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kVec<T>; ++i) run.s += __builtin_amdgcn_exp2f(run.at.exponent(x[i], scale));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        take_edges(part, run, l, scale, reach);
+        if (tid < 2) l.edges[tid] = 0;
+        const int more = REST && part.nvec > kKept ? part.nvec - kKept : 0;
+        if constexpr (REST)
+            stream<THREADS, kRestUnroll>(part.body() + kKept, more, [&](int v, u32x4 raw, bool inside) {
+                float x[kVec<T>];
+                unpack(inside ? raw : u32x4{lowest<T>(), lowest<T>(), lowest<T>(), lowest<T>()}, x);
+                uint8_t* byte = reinterpret_cast<uint8_t*>(marks) + kKept + v;
+                const uint32_t listed = a.tail && inside ? *byte : 0u;
+                if (listed) *byte = 0;
+                drop(x, listed);
+                add<false>(run, x, most_of(x), scale, reach);
+            });
+        if (a.tail) take_listed(part, run, t, scale, reach);
+        stores_done();
+        const Sums sums = block_sums<WAVES, false>(run, scale, l.sums);
+        if (listed_id >= 0) store(listed_grad, listed_id, listed_value);
+        const float loss = loss_of<WAVES>(a, t, sums, l);      // and every entry's logit is read
+        if (tid == 0 && a.loss) a.loss[r] = loss;
+        const Grad g(a, t, sums, w);
+        listed_id = t.id;
+        listed_value = g.listed(t, scale);
+        listed_grad = grad;
+        T* body = grad + part.head;
+        const bool whole = (reinterpret_cast<uintptr_t>(body) & 15u) == 0;
+        g.edges(a.l, part, grad);
+        r = next_row(r + gridDim.x);
+        Part<T> next = part;
+        if (r < a.l.rows) {
+            next = part_of(r);
+            e = entry_of(a, r);
+        } else {
+            next.nvec = 0;
+        }
+        if constexpr (REST)
+            stream<THREADS, kRestUnroll>(part.body() + kKept, more, [&](int v, u32x4 raw, bool inside) {
+                if (inside) g.vector(body + kKept * kVec<T>, v, raw, whole, scale);
+            });
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const uint32_t at = place(), v = u * THREADS + at;
+            const u32x4 raw = vector(u);
+            if (u * THREADS < next.nvec) fetch(next, u, at);
+            if (static_cast<int>(v) < part.nvec) g.vector(body, v, raw, whole, scale);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (r >= a.l.rows) break;
     }
+    stores_done();
+    __syncthreads();
+    if (listed_id >= 0) store(listed_grad, listed_id, listed_value);
 }
 
 // ---- launches ----------------------------------------------------------------------
@@ -850,11 +1088,35 @@ hipError_t scores(const ScoreArgs& a, const OpsDevice& d, hipStream_t stream)
     return hipSuccess;
 }
 
+// The gradient with rows in registers, if there are rows enough to keep the device busy.
+// False: it is not for these sizes.
+template <class T, int THREADS, int NV, bool REST>
+void resident(const DistillArgs& a, const OpsDevice& d, hipStream_t stream)
+{
+    const int64_t blocks = int64_t{d.cus} * (1024 / THREADS);
+    const int nvec = a.l.vocab / kVec<T> > THREADS * NV ? a.l.vocab / kVec<T> : THREADS * NV;
+    hipLaunchKernelGGL((resident_kernel<T, THREADS, NV, REST>), dim3(static_cast<unsigned>(a.l.rows < blocks ? a.l.rows : blocks)),
+                       dim3(THREADS), mark_words(nvec) * 4, stream, a);
+}
+
+template <class T> bool resident_grad(const DistillArgs& a, const OpsDevice& d, hipStream_t stream)
+{
+    const int nvec = a.l.vocab / kVec<T>;
+    if (!a.grad || a.l.rows < d.cus) return false;
+    if (nvec <= 256 * 8) resident<T, 256, 8, false>(a, d, stream);
+    else if (nvec <= 256 * 16) resident<T, 256, 16, false>(a, d, stream);
+    else if (nvec <= 512 * 16) resident<T, 512, 16, false>(a, d, stream);
+    else if (nvec <= 1024 * 16) resident<T, 512, 16, true>(a, d, stream);
+    else return false;
+    return true;
+}
+
 template <class T>
 hipError_t distill(const DistillArgs& a, const OpsDevice& d, hipStream_t stream)
 {
+    if (resident_grad<T>(a, d, stream)) return hipGetLastError();
     const Split s = split_rows<T>(a.l.rows, a.l.vocab, d.cus);
-    const size_t marks = a.tail ? static_cast<size_t>(mark_words(s.len / kVec<T> + 1)) * 4 : 0;
+    const size_t marks = static_cast<size_t>(mark_words(s.len / kVec<T>)) * 4;
     PartSums* sums = static_cast<PartSums*>(d.scratch);
     if (s.parts == 1) {
         hipLaunchKernelGGL((distill_kernel<T, kSums | kRest>), dim3(static_cast<unsigned>(a.l.rows)), dim3(kThreads), marks,
@@ -869,7 +1131,7 @@ hipError_t distill(const DistillArgs& a, const OpsDevice& d, hipStream_t stream)
         hipLaunchKernelGGL((distill_kernel<T, kSums>), grid, dim3(kThreads), marks, stream, a, r, s.parts, s.len, sums, x);
         // The loss alone is one block's a row.
         const int rest = a.grad ? s.parts : 1;
-        hipLaunchKernelGGL((distill_kernel<T, kRest>), dim3(static_cast<unsigned>(n * rest)), dim3(kThreads), 0, stream, a,
+        hipLaunchKernelGGL((distill_kernel<T, kRest>), dim3(static_cast<unsigned>(n * rest)), dim3(kThreads), marks, stream, a,
                            r, s.parts, s.len, sums, x);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

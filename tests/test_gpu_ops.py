@@ -497,6 +497,31 @@ def test_scan_steps_in_place_are_the_whole(torch, G, dt):
     assert float((h - last).abs().max()) < 1e-5
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("ragged,lengths", [(False, [40] * 3), (True, [300, 0, 1, 16, 40, 0, 7, 2000, 3]),
+                                            (True, [0, 5000, 0]), (False, [4096] * 2), (True, [9000, 64, 20000])])
+def test_scan_of_long_sequences_keeps_a_state_in_place(torch, G, ragged, lengths, dt):
+    """h_last in h0's memory: the same bits as with a memory of its own, also where other blocks
+    hold a sequence's first tokens and its last."""
+    D, B = 137, len(lengths)
+    off = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int64)
+    N = int(off[-1])
+    rng = np.random.default_rng(16)
+    x, _ = _matrix(torch, rng.normal(size=(N, D)), dt)
+    g, _ = _matrix(torch, rng.normal(size=(N, D)) + 4, dt)
+    start = torch.from_numpy(rng.normal(size=(B, D)).astype(np.float32)).cuda()
+    offs = torch.from_numpy(off).cuda()
+    y, y2 = (torch.zeros(N, D, device="cuda", dtype=x.dtype) for _ in range(2))
+    last, state = torch.zeros(B, D, device="cuda"), start.clone()
+    args = dict(x=x.data_ptr(), gate=g.data_ptr(), tokens=N, channels=D, sequences=B, dtype=DT[dt],
+                offsets=offs.data_ptr() if ragged else None)
+    with G.Ops(G.gem_scan_scratch(N, D)) as ops:
+        ops.scan_forward(y=y.data_ptr(), h0=start.data_ptr(), h_last=last.data_ptr(), **args)
+        ops.scan_forward(y=y2.data_ptr(), h0=state.data_ptr(), h_last=state.data_ptr(), **args)
+        torch.cuda.synchronize()
+    assert torch.equal(y, y2) and torch.equal(state, last)
+
+
 def test_scan_long_sequence(torch, G):
     """Long enough that thousands of parts of the sequence are joined."""
     _check_scan(torch, G, [40000, 3, 20001], 65, "bf16", gate=(5.0, 2.0))
@@ -605,6 +630,23 @@ def test_a_captured_graph_replays(torch, G):
             torch.cuda.synchronize()
             for n, t in o.items():
                 assert torch.equal(t, got[n]), (step, n)
+
+
+# ---- the ends of the ranges ---------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300007, 1 << 22])
+def test_scores_of_the_largest_vocabularies(torch, G, V, dt):
+    """Rows in as many parts as there are, with the most alternatives."""
+    rng = np.random.default_rng(17)
+    _check_scores(torch, G, rng.normal(size=(2, V)) * 2, dt, k=128, n=3)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_distill_of_the_largest_vocabulary(torch, G, dt):
+    rng = np.random.default_rng(18)
+    V = 1 << 22
+    ids, lp = _teacher(rng, 2, V, 128, mass=0.9)
+    _check_distill(torch, G, rng.normal(size=(2, V)) * 2, ids, lp, dt, tail=1)
 
 
 # ---- refusals ----------------------------------------------------------------------

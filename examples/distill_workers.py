@@ -146,7 +146,7 @@ def main():
     p.add_argument("--steps", type=int, default=120)
     p.add_argument("--workers", type=int, default=4)
     a = p.parse_args()
-    losses, student = train(a.steps, a.workers)
+    losses, student = train(a.steps, a.workers, lr=1.0)
     for i in range(0, len(losses), max(1, len(losses) // 6)):
         print(f"commit {i}: divergence from the teacher {losses[i]:.4f}")
     print(f"commit {len(losses) - 1}: {losses[-1]:.4f}")

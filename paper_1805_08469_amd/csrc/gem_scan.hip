@@ -9,7 +9,7 @@
 // inside a launch: no row needs another's result.  Bytes bound it.
 //
 // (One launch that reads everything once, its blocks handing states to each other through
-// memory, was slower: 168 us where this takes 145, 32768 x 2048 bfloat16 forward.  A
+// memory, was slower: 168 us where this takes 137, 32768 x 2048 bfloat16 forward.  A
 // state travels along a slice of channels at 4 tiles of 112 tokens a microsecond, by polls
 // that each take about one.)
 //
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(kThreads) void backward_map_kernel(const ScanBackAr
 // The gradients, kStep tokens at a time from the run's last: h from the state that forward
 // kept for them, then e from behind.  Keeping every eighth state costs a sixteenth of the
 // traffic, and saves walking from the run's first token or keeping h in the inputs' type.
-// Forward and backward of 32768 x 2048 bfloat16 take 346 us in their six launches (the bytes
+// Forward and backward of 32768 x 2048 bfloat16 take 337 us in their six launches (the bytes
 // alone, with x read three times and the gate four, 266 us at a copy's rate).
 template <class T, int KIND>
 __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const ScanBackArgs a, const Runs runs, const Bounds bound)
@@ -657,16 +657,29 @@ hipError_t pass_all(const gem_scan& s, const float* from, float* to, hipStream_t
     return hipGetLastError();
 }
 
-// Tokens of a run.
-int run_len(int64_t tokens) { return tokens >= 8192 ? 64 : tokens >= 2048 ? 32 : 16; }
+// Tokens of a run: the most, up to 128, that leave the launches `least` rows of 32 lanes (eight
+// to a compute unit at 2048).  Longer runs have fewer maps to write, join and read; fewer rows
+// leave compute units idle.  us, by runs of 128 / 64 / 32: 32768 x 2048 bfloat16, both
+// directions, 337 / 347 / 379; 65536 x 512 binary32 324 / 343 / 360; 16384 x 512 bfloat16 in
+// two sequences 150 / 102 / 83 (512, 1024 and 2048 rows).  Forward, packed sequences are
+// better with twice the rows, since a row in which they begin is walked token by token: 24 of
+// 16384 x 2048 93 / 88 / 90 (2048, 4096 and 8192 rows); both directions of 8192 x 4096 are 189
+// with 2048 rows, 200 with 4096.
+constexpr int64_t kForwardRows = 4096, kBackwardRows = 2048;
+int run_len(int64_t tokens, int64_t slices, int64_t least)
+{
+    int len = 128;
+    while (len > 16 && over(tokens, len) * slices < least) len /= 2;
+    return len;
+}
 static_assert(16 % kStateTokens == 0, "runs begin where states are kept");
 
-template <class T> Runs runs_of(const gem_scan& s, const OpsDevice& d)
+template <class T> Runs runs_of(const gem_scan& s, const OpsDevice& d, int64_t least)
 {
     Runs r;
-    r.len = run_len(s.tokens);
-    r.count = static_cast<int>(over(s.tokens, r.len));
     r.slices = static_cast<int>(over(s.channels, kSlice<T>));
+    r.len = run_len(s.tokens, r.slices, least);
+    r.count = static_cast<int>(over(s.tokens, r.len));
     r.maps = static_cast<float*>(d.scan);
     r.reach = r.maps + static_cast<int64_t>(r.count) * 2 * s.channels;
     r.in_place = false;
@@ -684,7 +697,7 @@ template <bool UP> void fold(const Runs& r, int channels, hipStream_t stream)
 template <class T, int KIND>
 hipError_t forward(const ScanArgs& a, const OpsDevice& d, hipStream_t stream)
 {
-    Runs r = runs_of<T>(a.s, d);
+    Runs r = runs_of<T>(a.s, d, kForwardRows);
     if (!a.s.offsets && a.s.tokens == a.s.sequences) {
         hipLaunchKernelGGL((step_kernel<T, KIND>), loop_grid(over(a.s.tokens * r.slices, kRows)), dim3(kThreads), 0, stream, a,
                            r.slices);
@@ -707,7 +720,7 @@ hipError_t forward(const ScanArgs& a, const OpsDevice& d, hipStream_t stream)
 template <class T, int KIND>
 hipError_t backward(const ScanBackArgs& a, const OpsDevice& d, hipStream_t stream)
 {
-    const Runs r = runs_of<T>(a.s, d);
+    const Runs r = runs_of<T>(a.s, d, kBackwardRows);
     const Bounds b = bounds_of(a.s);
     if (r.count > 1) {
         hipLaunchKernelGGL((backward_map_kernel<T, KIND>), grid_of(r), dim3(kThreads), 0, stream, a, r, b);
@@ -739,12 +752,17 @@ template <class T, class F, class A> hipError_t by_channels(const A& a, const Op
 
 }  // namespace
 
-// Rows of the launches (of the type with the narrower slices).
-int64_t scan_rows(int64_t tokens, int64_t channels) { return over(tokens, run_len(tokens)) * over(channels, kSlice<float>); }
+// The most rows of a launch (of the type with the narrower slices).
+int64_t scan_rows(int64_t tokens, int64_t channels)
+{
+    const int64_t slices = over(channels, kSlice<float>);
+    return over(tokens, run_len(tokens, slices, kForwardRows)) * slices;
+}
 
+// For the most runs: of the type with the wider slices, in the direction with the shorter runs.
 int64_t scan_scratch_bytes(int64_t tokens, int64_t channels)
 {
-    const int64_t runs = over(tokens, run_len(tokens));
+    const int64_t runs = over(tokens, run_len(tokens, over(channels, kSlice<uint16_t>), kForwardRows));
     return runs <= 1 ? 0 : runs * channels * 3 * static_cast<int64_t>(sizeof(float));
 }
 

@@ -427,6 +427,8 @@ typedef struct gem_ops_handle gem_ops_t;
 /* Largest vocabulary, and the most alternatives of a row. */
 #define GEM_VOCAB_MAX (1 << 22)
 #define GEM_TOP_MAX 128
+/* Most tokens of a recurrence. */
+#define GEM_TOKENS_MAX 2147483392
 
 /* Create the handle on the current device.  stream is the hipStream_t its work
  * is queued on (NULL: the device's null stream) and must outlive it.
@@ -510,7 +512,7 @@ int gem_distill_grad(gem_ops_t* ops, const gem_logits* z, const gem_teacher* tea
                      const float* weight, float* loss, void* grad, int64_t grad_stride);
 
 /* Inputs of the gated linear recurrence over `sequences` (>= 1) sequences of
- * tokens x channels, packed one after the other:
+ * tokens (0 to GEM_TOKENS_MAX) x channels, packed one after the other:
  *     a_t = sigmoid(gate_t);  h_t = a_t h_{t-1} + (1 - a_t) x_t
  * for each channel, from h0 ([sequences][channels] binary32; NULL: zeros).
  * offsets ([sequences + 1] on the device, rising from 0 to tokens) gives each

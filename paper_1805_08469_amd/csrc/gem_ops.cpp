@@ -26,10 +26,9 @@ namespace {
     } while (0)
 
 // Most rows of logits (a launch of a block a row stays within the 2^32 threads of a
-// dispatch), most tokens of a recurrence, and the largest row stride in elements: their
-// products and every byte offset formed from them stay within 63 bits.
+// dispatch), and the largest row stride in elements: products of these, of
+// GEM_TOKENS_MAX and of elements' sizes stay within 63 bits.
 constexpr int64_t kRowsMax = int64_t{1} << 22;
-constexpr int64_t kTokensMax = INT32_MAX;
 constexpr int64_t kStrideMax = int64_t{1} << 28;
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -69,7 +68,7 @@ int check_scan(const gem_scan* s, gem_scan* out)
 {
     if (!s) return GEM_EINVAL;
     if (s->dtype != GEM_F32 && s->dtype != GEM_BF16) return GEM_EDTYPE;
-    if (s->tokens < 0 || s->tokens > kTokensMax || s->channels < 1 || s->sequences < 1)
+    if (s->tokens < 0 || s->tokens > GEM_TOKENS_MAX || s->channels < 1 || s->sequences < 1)
         return GEM_EINVAL;
     *out = *s;
     if (!row_stride(s->x_stride, s->channels, &out->x_stride)) return GEM_EINVAL;
@@ -198,14 +197,14 @@ int gem_distill_grad(gem_ops_t* ops, const gem_logits* z, const gem_teacher* tea
 
 int gem_scan_scratch(int64_t tokens, int32_t channels, int64_t* bytes)
 {
-    if (!bytes || tokens < 0 || tokens > kTokensMax || channels < 1) return GEM_EINVAL;
+    if (!bytes || tokens < 0 || tokens > GEM_TOKENS_MAX || channels < 1) return GEM_EINVAL;
     *bytes = gemk::scan_scratch_bytes(tokens, channels);
     return GEM_OK;
 }
 
 int gem_scan_state_rows(int64_t tokens, int64_t* rows)
 {
-    if (!rows || tokens < 0 || tokens > kTokensMax) return GEM_EINVAL;
+    if (!rows || tokens < 0 || tokens > GEM_TOKENS_MAX) return GEM_EINVAL;
     *rows = (tokens + gemk::kStateTokens - 1) / gemk::kStateTokens;
     return GEM_OK;
 }

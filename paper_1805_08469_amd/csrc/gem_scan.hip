@@ -28,6 +28,8 @@ constexpr int kThreads = 256;
 constexpr int kLanes = 32;                 // lanes of a row
 constexpr int kRows = kThreads / kLanes;   // rows of a block
 constexpr int kStep = kStateTokens;        // tokens that a lane loads at a time
+// Tokens are counted in ints, and walks look up to three steps past the last one.
+static_assert(GEM_TOKENS_MAX <= INT32_MAX - 3 * kStep, "positions of tokens fit an int");
 
 template <class T> constexpr int kChan = 8 / static_cast<int>(sizeof(T));   // channels of a lane
 template <class T> constexpr int kSlice = kLanes * kChan<T>;                // and of a row

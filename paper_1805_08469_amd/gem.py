@@ -41,6 +41,7 @@ GEM_P_MAX = 1 << 31
 GEM_PI_BINS = 643
 GEM_VOCAB_MAX = 1 << 22
 GEM_TOP_MAX = 128
+GEM_TOKENS_MAX = (1 << 31) - 256
 
 # Every symbol include/gem.h declares.
 EXPORTED = (

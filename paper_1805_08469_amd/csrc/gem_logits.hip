@@ -27,9 +27,9 @@ constexpr float kLeast = -200.0f;
 
 // Where exponents (x - ref) scale are taken from.  Fused, they are x scale - rc with
 // rc = ref scale rounded, which puts them all off by the rounding's error, skew: sums are
-// freed of it when they are moved to another reference.  Near the type's ends (a row
-// masked by the lowest value) a logit's own multiple overflows: there (wide) the
-// difference comes first.
+// freed of it when they are moved to another reference.  From 2^24 on (a row masked by a
+// large value) the error is more than half an octave, and further out it leaves the
+// exponent's range: there (wide) the difference comes first.
 struct Reference {
     float ref = -kInf, rc = 0.0f;
     bool wide = false;
@@ -38,7 +38,7 @@ struct Reference {
     {
         ref = at;
         rc = at * scale;
-        wide = !(__builtin_fabsf(rc) < 0x1p120f);
+        wide = !(__builtin_fabsf(rc) < 0x1p24f);
     }
     __device__ float skew(float scale) const
     {

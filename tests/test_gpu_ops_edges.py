@@ -1,0 +1,71 @@
+"""The worker's operators where values leave the ordinary: records without mass, tails far below
+the listed tokens, masks of any size, NaN, and what every call has to leave behind."""
+import math
+
+import numpy as np
+import pytest
+
+import ops_reference as R
+from test_gpu_ops import DT, G, INF, _check_distill, _check_scores, _host, _matrix, _same, _score, _teacher, torch  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- masks -----------------------------------------------------------------------
+MASKS = [-1e9, -3e9, -1e10, -7e12, -1e30, -3e35]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [700, 20001, 150001])
+def test_scores_of_rows_masked_by_any_finite_value(torch, G, V, dt):
+    """Whole threads, parts and rows of logits far below the others, where no multiple of a
+    logit is exact any more."""
+    rng = np.random.default_rng(V)
+    for T in (1.0, 0.5):
+        z = rng.normal(size=(4 * len(MASKS), V)) * 2
+        for i, m in enumerate(MASKS):
+            z[4 * i, :V // 2] = m
+            z[4 * i + 1, V // 3:] = m
+            z[4 * i + 2, np.arange(V) != V - 2] = m
+            z[4 * i + 3, :] = m
+        _check_scores(torch, G, z, dt, T=T, k=8, n=3, what=f"masked T={T}")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(24, 700), (24, 20001), (24, 150001), (288, 5001), (264, 40001)])
+def test_distill_of_rows_masked_by_any_finite_value(torch, G, rows, V, dt):
+    rng = np.random.default_rng(V + rows)
+    ids, lp = _teacher(rng, rows, V, 16)
+    values = rng.normal(size=(rows, V)) * 2
+    free = np.ones((rows, V), bool)
+    for i in range(rows):
+        if i % 4 == 0:
+            free[i, :V // 2] = False
+        elif i % 4 == 1:
+            free[i, V // 3:] = False
+        elif i % 4 == 2:
+            free[i, rng.random(V) < 0.9] = False
+        free[i, ids[i]] = True
+        values[i, ~free[i]] = MASKS[i // 4 % len(MASKS)]
+        if i % 24 == 3:
+            values[i, :] = MASKS[i // 24 % len(MASKS)]
+    z, _ = _matrix(torch, values, dt)
+    ti, tl = torch.from_numpy(ids).cuda(), torch.from_numpy(lp).cuda()
+    loss, loss2 = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    g = torch.zeros(rows, V, device="cuda", dtype=z.dtype)
+    print(f"[distill] masked rows={rows} V={V} {dt}", flush=True)
+    args = dict(ids=ti.data_ptr(), teacher=tl.data_ptr(), k=16, tail=0, temperature=0.5)
+    with G.Ops() as ops:
+        ops.distill_loss(z.data_ptr(), rows, V, DT[dt], loss=loss.data_ptr(), **args)
+        ops.distill_grad(z.data_ptr(), rows, V, DT[dt], loss=loss2.data_ptr(), grad=g.data_ptr(), **args)
+        torch.cuda.synchronize()
+    host, got, got2, grad = _host(z), _host(loss), _host(loss2), _host(g)
+    for r in range(rows):
+        lo, gr, q, p, pt, qt = R.distill_row(host[r], 0.5, ids[r], lp[r], 0)
+        # A masked logit's distance from the others is a difference that rounds once and that
+        # nothing is read from: the spread that enters the bounds is that of the free ones.
+        level = np.where(free[r], host[r], -INF) if r % 24 != 3 else np.zeros(V)
+        lt, gt = R.distill_tolerance(V, 16, 0.5, level, q, p, pt, qt, lo, gr, 1.0, dt == "bf16")
+        _same(got[r:r + 1], np.array([lo]), lt, f"loss of row {r}")
+        _same(got2[r:r + 1], np.array([lo]), lt, f"loss (with gradient) of row {r}")
+        _same(grad[r], gr, gt, f"gradient of row {r}")

@@ -503,9 +503,11 @@ int gem_distill_loss(gem_ops_t* ops, const gem_logits* z, const gem_teacher* tea
 
 /* The same and its gradient: grad (rows x vocab of the logits' type,
  * grad_stride elements between rows) receives
- *     weight[r] / temperature * (q_v - p_v)               for a listed token
- *     weight[r] / temperature * q_v (1 [- p_t / q_t])     for another,
- * zero in rows of weight 0.  loss may be NULL.  grad may be the logits' own
+ *     weight[r] / temperature * (m q_v - p_v)             for a listed token
+ *     weight[r] / temperature * q_v (m [- p_t / q_t])     for another,
+ * zero in rows of weight 0.  m is the mass of the record, sum_i p_i [+ p_t]: 1, but
+ * 0 where no entry has a probability (tail 0), and the sum of p_i where that
+ * exceeds 1 (tail 1).  loss may be NULL.  grad may be the logits' own
  * memory (same address and stride).  A row of logits that are all -inf has
  * loss +inf and q = 0 in its gradient.  Errors: EINVAL, EDTYPE, EALIGN. */
 int gem_distill_grad(gem_ops_t* ops, const gem_logits* z, const gem_teacher* teacher,

@@ -624,11 +624,11 @@ __device__ __forceinline__ int distinct(const Entry& e, int k, DistillLds& l)
     return again ? -1 : e.id;
 }
 
-// Thread i's entry as it counts: its token (-1: none), log probability and probability, and
-// p_t; and the token's logit.
+// Thread i's entry as it counts: its token (-1: none), log probability and probability; the
+// row's p_t and mass, the sum of all p and p_t; and the token's logit.
 struct Teacher {
     int id = -1;
-    float lp = 0.0f, p = 0.0f, pt = 0.0f, x = -kInf;
+    float lp = 0.0f, p = 0.0f, pt = 0.0f, mass = 0.0f, x = -kInf;
 };
 
 template <int WAVES>
@@ -640,13 +640,16 @@ __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const Entry&
     if (a.tail) {
         t.lp = lp;
         t.p = t.id >= 0 ? expf(lp) : 0.0f;
-        t.pt = __builtin_fmaxf(0.0f, 1.0f - block_sum<WAVES>(t.p, l.red));
+        const float sum = block_sum<WAVES>(t.p, l.red);
+        t.pt = __builtin_fmaxf(0.0f, 1.0f - sum);
+        t.mass = __builtin_fmaxf(1.0f, sum);
     } else {
         const float top = block_max<WAVES>(lp, l.red);
         t.p = t.id >= 0 && top > -kInf ? expf(lp - top) : 0.0f;
         const float sum = block_sum<WAVES>(t.p, l.red);
         t.lp = lp - (top + logf(sum));
         t.p = sum > 0.0f ? t.p / sum : 0.0f;
+        t.mass = sum > 0.0f ? 1.0f : 0.0f;
     }
     return t;
 }
@@ -710,7 +713,8 @@ __device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t,
     return loss;
 }
 
-// A row's gradient: c 2^d of unlisted tokens, and of a listed one f (2^d inv - p).  Every
+// A row's gradient: c 2^d of unlisted tokens, and of a listed one f (2^d inv - p), with inv
+// the record's mass over the sum of exponentials.  Every
 // element is stored as an unlisted token's, and the listed ones again when those stores are
 // done (stores_done), which spares the vectors a look at the marks.
 struct Grad {
@@ -722,7 +726,7 @@ struct Grad {
         at.set(u.ref, a.l.scale);
         f = w * a.l.inv_t;
         const float all = u.s + u.t;
-        inv = all == 0.0f ? 0.0f : 1.0f / all;
+        inv = all == 0.0f ? 0.0f : t.mass / all;
         const float rest = t.pt > 0.0f && u.s != 0.0f ? t.pt / u.s : 0.0f;
         c = f * (inv - rest) * __builtin_amdgcn_exp2f(-at.skew(a.l.scale));
     }

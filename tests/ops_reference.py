@@ -86,11 +86,12 @@ def distill_row(z, T, ids, lp, tail):
         out[at] = False
         pt = max(0.0, 1.0 - p.sum()) if tail else 0.0
         qt = q[out].sum()
-        g = q - full
+        mass = p.sum() + pt
+        g = mass * q - full
         if pt > 0:
             loss += pt * (np.log(pt) - np.log(qt))
             if qt > 0:
-                g[out] = q[out] * (1 - pt / qt)
+                g[out] = q[out] * (mass - pt / qt)
     return loss, g / T, q, full, pt, qt
 
 

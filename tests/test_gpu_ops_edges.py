@@ -69,3 +69,54 @@ def test_distill_of_rows_masked_by_any_finite_value(torch, G, rows, V, dt):
         _same(got[r:r + 1], np.array([lo]), lt, f"loss of row {r}")
         _same(got2[r:r + 1], np.array([lo]), lt, f"loss (with gradient) of row {r}")
         _same(grad[r], gr, gt, f"gradient of row {r}")
+
+
+# ---- what a record holds ------------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(6, 40), (3, 90001), (300, 3001)])
+def test_distill_rows_without_entries_have_no_gradient(torch, G, rows, V, dt):
+    """Their loss is 0 whatever the logits are."""
+    rng = np.random.default_rng(21)
+    ids, lp = _teacher(rng, rows, V, 7)
+    ids[::3] = -1
+    ids[1::3] = V
+    lp[2::3] = -INF
+    z, _ = _matrix(torch, rng.normal(size=(rows, V)), dt)
+    ti, tl = torch.from_numpy(ids).cuda(), torch.from_numpy(lp).cuda()
+    for tail in (0, 1):
+        loss, g = torch.full((rows,), 55.0, device="cuda"), torch.full((rows, V), 33.0, device="cuda", dtype=z.dtype)
+        with G.Ops() as ops:
+            ops.distill_grad(z.data_ptr(), rows, V, DT[dt], ids=ti.data_ptr(), teacher=tl.data_ptr(), k=7, tail=tail,
+                             loss=loss.data_ptr(), grad=g.data_ptr())
+            torch.cuda.synchronize()
+        empty = slice(None) if tail == 0 else [r for r in range(rows) if r % 3 != 2]
+        # with a tail all mass is the tail's, and its gradient is q (1 - 1 / 1)
+        assert float(loss[empty].abs().max()) <= (0 if tail == 0 else 4 * R.U)
+        assert float(g[empty].float().abs().max()) <= (0 if tail == 0 else 8 * R.U)
+
+
+@pytest.mark.parametrize("over", [1.05, 1.5])
+def test_distill_gradient_of_records_of_any_mass_against_differences(torch, G, over):
+    """Probabilities that sum to more than 1, against central differences of the loss in 64 bits."""
+    rng = np.random.default_rng(22)
+    V, step = 29, 1e-5
+    ids, lp = _teacher(rng, 1, V, 6, mass=over)
+    z = (rng.normal(size=(1, V))).astype(np.float32).astype(np.float64)
+    zt, _ = _matrix(torch, z, "f32")
+    g = torch.zeros(1, V, device="cuda")
+    ti, tl = torch.from_numpy(ids).cuda(), torch.from_numpy(lp).cuda()
+    with G.Ops() as ops:
+        ops.distill_grad(zt.data_ptr(), 1, V, 0, ids=ti.data_ptr(), teacher=tl.data_ptr(), k=6, tail=1, grad=g.data_ptr())
+        torch.cuda.synchronize()
+
+    def loss(z):
+        e = np.exp(z - z.max())
+        logq = np.log(e / e.sum())[ids[0]]
+        return float((np.exp(lp[0].astype(np.float64)) * (lp[0] - logq)).sum())
+
+    for v in range(V):
+        hi, lo = z[0].copy(), z[0].copy()
+        hi[v] += step
+        lo[v] -= step
+        d = (loss(hi) - loss(lo)) / (2 * step)
+        assert abs(d - float(g[0, v])) < 2e-5 * max(abs(d), 0.05), v

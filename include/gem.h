@@ -493,8 +493,10 @@ typedef struct {
 /* Distillation loss of each row: the Kullback-Leibler divergence
  *     loss = sum_i p_i (log p_i - log q_{id_i})  [+ p_t (log p_t - log q_t)]
  * of q = softmax(logits / temperature) from the teacher's p; with tail, p_t =
- * max(0, 1 - sum_i p_i) and q_t = sum of q over unlisted tokens.  Outcomes with
- * p = 0 add nothing; a row without entries has loss 0.  weight ([rows], NULL:
+ * max(0, 1 - sum_i p_i) and q_t = sum of q over unlisted tokens (0 where it is
+ * below 2^-1022, as for tokens masked by a large finite logit: the loss is then
+ * infinite, and the tail has no part in the gradient).  Outcomes with p = 0 add
+ * nothing; a row without entries has loss 0.  weight ([rows], NULL:
  * all 1) is the factor of the row's loss in what is minimised: it does not
  * multiply loss[r], but a row of weight 0 (padding) has loss 0 and its logits
  * are not read.  Errors: EINVAL, EDTYPE, EALIGN. */

@@ -50,8 +50,7 @@ struct Reference {
     }
 };
 
-// A thread's s = sum 2^d and beside it t: sum 2^d d (SUM_D), or a second sum of
-// exponentials.
+// A thread's s = sum 2^d and, with SUM_D, t = sum 2^d d.
 struct Run {
     Reference at;
     float limit = -kInf;       // a logit above it moves the reference
@@ -59,14 +58,13 @@ struct Run {
     float s = 0.0f, t = 0.0f;
 };
 
-// Sums moved so that every d grows by d.
+// Sums moved so that every d grows by d (t with SUM_D).
 template <bool SUM_D>
 __device__ __forceinline__ void shift_sums(float& s, float& t, float d)
 {
     d = __builtin_fmaxf(d, kLeast);
     const float c = __builtin_amdgcn_exp2f(d);
     if constexpr (SUM_D) t = c * __builtin_fmaf(s, d, t);
-    else t *= c;
     s *= c;
 }
 
@@ -104,18 +102,18 @@ __device__ __forceinline__ void add(Run& r, const float (&x)[N], float most, flo
     }
 }
 
-// A row's (or a part's) sums about the largest of its references; ref is 0 where
+// Scores: a row's (or a part's) sums about the largest of its references; ref is 0 where
 // no logit is above -inf.
 struct Sums {
     float ref, s, t;
 };
 
-template <int WAVES, bool SUM_D>
+template <int WAVES>
 __device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*lds)[4])
 {
     const float top = wave_max(r.at.ref);
     float s = r.s, t = r.t;
-    if (r.at.ref > -kInf) shift_sums<SUM_D>(s, t, (r.at.ref - top) * scale - r.at.skew(scale));
+    if (r.at.ref > -kInf) shift_sums<true>(s, t, (r.at.ref - top) * scale - r.at.skew(scale));
     s = wave_sum(s);
     t = wave_sum(t);
     const int wave = threadIdx.x >> 6;
@@ -132,7 +130,7 @@ __device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*ld
     for (int w = 0; w < WAVES; ++w) {
         s = lds[w][1];
         t = lds[w][2];
-        if (lds[w][0] > -kInf) shift_sums<SUM_D>(s, t, (lds[w][0] - out.ref) * scale);
+        if (lds[w][0] > -kInf) shift_sums<true>(s, t, (lds[w][0] - out.ref) * scale);
         out.s += s;
         out.t += t;
     }
@@ -439,7 +437,7 @@ __device__ void select_top(TopLds& l, const Part<T>& part, const typename GroupK
 
 // What a part of a row leaves for the row's joining block.
 struct PartSums {
-    float ref, s, t, pad;
+    float ref, s, t, lref;
 };
 
 __device__ __forceinline__ float log_prob(const LogitArgs& a, float x, float ref, float ls)
@@ -522,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a, int6
             }
         }
     });
-    const Sums u = block_sums<kThreads / 64, true>(run, scale, lds);
+    const Sums u = block_sums<kThreads / 64>(run, scale, lds);
     if constexpr (TOP)
         select_top(top, part, keys, groups, order(high) >> shift, order(kVec<T> < kGroup ? seen : high) >> shift, a.top_k);
     if (parts == 1) {
@@ -560,7 +558,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const ScoreArgs a, int64
     const int n = parts * a.top_k;
     for (int j = tid; j < n; j += kThreads) keys[j] = tops[static_cast<int64_t>(blockIdx.x) * n + j];
     if (tid == 0) top.count = 0;
-    const Sums u = block_sums<kThreads / 64, true>(run, a.l.scale, lds);
+    const Sums u = block_sums<kThreads / 64>(run, a.l.scale, lds);
     if (a.top_k) {
         const int mine = tid < n ? (n - tid + kThreads - 1) / kThreads : 0;
         const auto key = [&](int j) { return keys[tid + j * kThreads]; };
@@ -680,6 +678,25 @@ template <int N> __device__ __forceinline__ void drop(float (&x)[N], uint32_t li
     for (int i = 0; i < N; ++i) x[i] = listed >> i & 1u ? -kInf : x[i];
 }
 
+// The same of a vector's bits.
+__device__ __forceinline__ u32x4 drop(u32x4 v, uint32_t listed, float)
+{
+    if (__builtin_expect(__ballot(listed != 0) == 0, 0)) return v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = listed >> i & 1u ? 0xFF800000u : v[i];
+    return v;
+}
+__device__ __forceinline__ u32x4 drop(u32x4 v, uint32_t listed, uint16_t)
+{
+    if (__builtin_expect(__ballot(listed != 0) == 0, 0)) return v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = listed >> 2 * i & 1u ? (v[i] & 0xFFFF0000u) | 0xFF80u : v[i];
+        v[i] = listed >> (2 * i + 1) & 1u ? (v[i] & 0xFFFFu) | 0xFF800000u : v[i];
+    }
+    return v;
+}
+
 // The head and the tail, without their marked elements.
 template <class T>
 __device__ __forceinline__ void take_edges(const Part<T>& part, Run& run, const DistillLds& l, float scale, float reach)
@@ -691,44 +708,119 @@ __device__ __forceinline__ void take_edges(const Part<T>& part, Run& run, const 
     add<false>(run, x, most_of(x), scale, reach);
 }
 
-// Listed tokens' exponentials are summed apart, in t, by their entries' threads.
-template <class T>
-__device__ __forceinline__ void take_listed(const Part<T>& part, Run& run, const Teacher& t, float scale, float reach)
+// With a tail, listed tokens' exponentials are summed apart, about a reference of their own:
+// unlisted ones may lie so far below that about a common one they are nothing, and p_t q_v / q_t
+// is of q_t's size whatever that is.  An entry's thread has one, about itself.
+struct Listed {
+    float ref = -kInf, t = 0.0f;
+};
+template <class T> __device__ __forceinline__ Listed listed_of(const Part<T>& part, const Teacher& t)
 {
-    const float x = t.id >= part.begin && t.id < part.begin + part.n ? t.x : -kInf;
-    rebase<false>(run, x, scale, reach);
-    run.t += __builtin_amdgcn_exp2f(run.at.exponent(x, scale));
+    Listed l;
+    if (t.id >= part.begin && t.id < part.begin + part.n) l.ref = t.x;
+    l.t = l.ref == -kInf ? 0.0f : 1.0f;
+    return l;
 }
+__device__ __forceinline__ float moved(float t, float ref, float to, float scale)
+{
+    return t == 0.0f ? 0.0f : t * __builtin_amdgcn_exp2f((ref - to) * scale);
+}
+
+// A row's (or a part's) sums: s of unlisted tokens (without a tail of all) about ref, t of listed
+// ones about lref; a reference is -inf where no logit is above it.
+template <int WAVES>
+__device__ __forceinline__ PartSums block_parts(const Run& r, Listed l, bool tail, float scale, float (*lds)[4])
+{
+    // Both halves step by step together: a step of one covers the wait for the other's.
+    float top = r.at.ref, ltop = l.ref;
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) {
+        const float a = __shfl_xor(top, m), b = __shfl_xor(ltop, m);
+        top = __builtin_fmaxf(top, a);
+        ltop = __builtin_fmaxf(ltop, b);
+    }
+    float s = r.s, none = 0.0f, t = moved(l.t, l.ref, ltop, scale);
+    if (r.at.ref > -kInf) shift_sums<false>(s, none, (r.at.ref - top) * scale - r.at.skew(scale));
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) {
+        const float a = __shfl_xor(s, m), b = __shfl_xor(t, m);
+        s += a;
+        t += b;
+    }
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+        lds[wave][0] = top;
+        lds[wave][1] = s;
+        lds[wave][2] = t;
+        lds[wave][3] = ltop;
+    }
+    __syncthreads();
+    PartSums out{lds[0][0], 0.0f, 0.0f, -kInf};
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) out.ref = __builtin_fmaxf(out.ref, lds[w][0]);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        s = lds[w][1];
+        if (lds[w][0] > -kInf) shift_sums<false>(s, none, (lds[w][0] - out.ref) * scale);
+        out.s += s;
+    }
+    if (tail) {
+        constexpr int kWaves = GEM_TOP_MAX / 64;       // that hold entries
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) out.lref = __builtin_fmaxf(out.lref, lds[w][3]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) out.t += moved(lds[w][2], lds[w][3], out.lref, scale);
+    }
+    return out;
+}
+static_assert(GEM_TOP_MAX % 64 == 0 && GEM_TOP_MAX <= kThreads, "whole waves hold a row's entries");
+
+// What loss and gradient take of a row's sums: the sum of all about top, log2 of it, and s about
+// ref.
+struct RowSums {
+    float ref, s, top, all, ls;
+
+    __device__ RowSums(const PartSums& p, float scale) : ref(p.ref), s(p.s)
+    {
+        top = __builtin_fmaxf(p.ref, p.lref);
+        if (top == -kInf) top = 0.0f;
+        if (ref == -kInf) ref = top;
+        all = moved(s, ref, top, scale) + moved(p.t, p.lref, top, scale);
+        ls = __builtin_log2f(all);
+    }
+    // log2 q_t.
+    __device__ float rest(float scale) const { return __builtin_log2f(s) + (ref - top) * scale - ls; }
+    // No unlisted token can occur: q_t is 0, or below the normal numbers of binary64, which a
+    // mask of any value counts as (its gap to the others is no quantity).
+    __device__ bool no_rest(float scale) const { return s == 0.0f || rest(scale) < -1022.0f; }
+};
 
 // The row's loss, from thread i's entry.
 template <int WAVES>
-__device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t, const Sums& u, DistillLds& l)
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t, const RowSums& u, DistillLds& l)
 {
-    const float all = u.s + u.t, ls = __builtin_log2f(all);
     float part = 0.0f;
-    if (t.p > 0.0f) part = t.p * (t.lp - log_prob(a.l, t.x, u.ref, ls));
+    if (t.p > 0.0f) part = t.p * (t.lp - log_prob(a.l, t.x, u.top, u.ls));
     float loss = block_sum<WAVES>(part, l.red);
-    if (t.pt > 0.0f)
-        loss += u.s == 0.0f ? kInf : t.pt * (logf(t.pt) - (__builtin_log2f(u.s) - ls) * kLn2);
+    if (t.pt > 0.0f) loss += u.no_rest(a.l.scale) ? kInf : t.pt * (logf(t.pt) - u.rest(a.l.scale) * kLn2);
     return loss;
 }
 
-// A row's gradient: c 2^d of unlisted tokens, and of a listed one f (2^d inv - p), with inv
-// the record's mass over the sum of exponentials.  Every
+// A row's gradient: c 2^d of unlisted tokens, about the reference of theirs, and of a listed one
+// f (2^d inv - p) about that of all, with inv the record's mass over the sum of exponentials.  Every
 // element is stored as an unlisted token's, and the listed ones again when those stores are
 // done (stores_done), which spares the vectors a look at the marks.
 struct Grad {
     Reference at;
-    float c, f, inv;
+    float c, f, inv, top;
 
-    __device__ Grad(const DistillArgs& a, const Teacher& t, const Sums& u, float w)
+    __device__ Grad(const DistillArgs& a, const Teacher& t, const RowSums& u, float w) : top(u.top)
     {
         at.set(u.ref, a.l.scale);
         f = w * a.l.inv_t;
-        const float all = u.s + u.t;
-        inv = all == 0.0f ? 0.0f : t.mass / all;
-        const float rest = t.pt > 0.0f && u.s != 0.0f ? t.pt / u.s : 0.0f;
-        c = f * (inv - rest) * __builtin_amdgcn_exp2f(-at.skew(a.l.scale));
+        inv = u.all == 0.0f ? 0.0f : t.mass / u.all;
+        const float rest = t.pt > 0.0f && !u.no_rest(a.l.scale) ? t.pt / u.s : 0.0f;
+        c = f * (moved(inv, u.ref, u.top, a.l.scale) - rest) * __builtin_amdgcn_exp2f(-at.skew(a.l.scale));
     }
 
     // Vector v of the part; whole: its rows are aligned as the logits'.
@@ -763,7 +855,7 @@ struct Grad {
 
     __device__ float listed(const Teacher& t, float scale) const
     {
-        return f * (__builtin_amdgcn_exp2f((t.x - at.ref) * scale) * inv - t.p);
+        return f * (__builtin_amdgcn_exp2f((t.x - top) * scale) * inv - t.p);
     }
 };
 
@@ -837,21 +929,22 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a, 
     if constexpr (STEP & kRest) t = teacher_of<WAVES>(a, e, l);
     else t.id = a.tail ? distinct(e, a.k, l) : e.id;
     if (t.id >= 0) t.x = STEP & kSums ? load(row, t.id) : part_x[i * a.k + tid];
-    Sums u{0.0f, 0.0f, 0.0f};
+    PartSums sums;
     Run run;
+    Listed listed;
     if constexpr (STEP & kSums) {
         const float reach = 20.0f / scale;
         if (a.tail) {
             mark(part, marks, l, t.id, [](int v) { return v; });
             __syncthreads();
             take_part<T, true>(part, run, marks, l, scale, reach);
-            take_listed(part, run, t, scale, reach);
+            listed = listed_of(part, t);
         } else {
             take_part<T, false>(part, run, marks, l, scale, reach);
         }
-        u = block_sums<WAVES, false>(run, scale, l.sums);
+        sums = block_parts<WAVES>(run, listed, a.tail, scale, l.sums);
         if constexpr (!(STEP & kRest)) {
-            if (tid == 0) part_sums[blockIdx.x] = PartSums{u.s + u.t == 0.0f ? -kInf : u.ref, u.s, u.t, 0.0f};
+            if (tid == 0) part_sums[blockIdx.x] = sums;
             if (t.id >= part.begin && t.id < part.begin + part.n) part_x[i * a.k + tid] = t.x;
             return;
         }
@@ -861,10 +954,11 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a, 
             run.at.ref = p.ref;    // its sums have no skew
             run.at.wide = true;
             run.s = p.s;
-            run.t = p.t;
+            listed = Listed{p.lref, p.t};
         }
-        u = block_sums<WAVES, false>(run, scale, l.sums);
+        sums = block_parts<WAVES>(run, listed, a.tail, scale, l.sums);
     }
+    const RowSums u(sums, scale);
     const float loss = loss_of<WAVES>(a, t, u, l);     // and every entry's logit is read
     if (a.loss && q == 0 && tid == 0) a.loss[r] = loss;
     if (!grad) return;
@@ -951,7 +1045,15 @@ __global__ __launch_bounds__(THREADS, 4) void resident_kernel(const DistillArgs 
         if (a.tail) mark(part, marks, l, e.id, byte_of);
         Teacher t = teacher_of<WAVES>(a, e, l);
         if (t.id >= 0) t.x = load(part.p, t.id);
-        // Sums, about the largest of the thread's vectors.
+        // Sums, about the largest of the thread's unlisted elements.
+        uint32_t words[NV / 4] = {};
+        if (a.tail) {
+#pragma unroll
+            for (int i = 0; i < NV / 4; ++i) {
+                words[i] = marks[tid * (NV / 4) + i];
+                marks[tid * (NV / 4) + i] = 0;
+            }
+        }
         float most = -kInf;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
@@ -961,6 +1063,7 @@ __global__ __launch_bounds__(THREADS, 4) void resident_kernel(const DistillArgs 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) d[u][i] = inside ? d[u][i] : lowest<T>();
                 }
+                d[u] = drop(d[u], words[u / 4] >> u % 4 * 8 & 0xFFu, T{});
                 float x[kVec<T>];
                 unpack(vector(u), x);
                 most = max3(most, most_of(x), most);
@@ -969,20 +1072,11 @@ __global__ __launch_bounds__(THREADS, 4) void resident_kernel(const DistillArgs 
         }
         Run run;
         rebase<false>(run, most, scale, reach);
-        uint32_t words[NV / 4] = {};
-        if (a.tail) {
-#pragma unroll
-            for (int i = 0; i < NV / 4; ++i) {
-                words[i] = marks[tid * (NV / 4) + i];
-                marks[tid * (NV / 4) + i] = 0;
-            }
-        }
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
             if (u * THREADS < part.nvec) {
                 float x[kVec<T>];
                 unpack(vector(u), x);
-                drop(x, words[u / 4] >> u % 4 * 8 & 0xFFu);
                 if (__builtin_expect(!run.wide, 1)) {
 #pragma unroll
                     for (int i = 0; i < kVec<T>; ++i) run.s += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -run.at.rc));
@@ -1006,9 +1100,10 @@ __global__ __launch_bounds__(THREADS, 4) void resident_kernel(const DistillArgs 
                 drop(x, listed);
                 add<false>(run, x, most_of(x), scale, reach);
             });
-        if (a.tail) take_listed(part, run, t, scale, reach);
+        Listed listed;
+        if (a.tail) listed = listed_of(part, t);
         stores_done();
-        const Sums sums = block_sums<WAVES, false>(run, scale, l.sums);
+        const RowSums sums(block_parts<WAVES>(run, listed, a.tail, scale, l.sums), scale);
         if (listed_id >= 0) store(listed_grad, listed_id, listed_value);
         const float loss = loss_of<WAVES>(a, t, sums, l);      // and every entry's logit is read
         if (tid == 0 && a.loss) a.loss[r] = loss;
@@ -1070,7 +1165,8 @@ Split split_rows(int64_t rows, int vocab, int cus)
     if (len > kPartMax<T>) len = kPartMax<T>;
     return {(vocab + len - 1) / len, len};
 }
-static_assert(GEM_VOCAB_MAX / kPartMax<float> <= kPartsMax, "a row's parts are joined by one block");
+static_assert(GEM_VOCAB_MAX / kPartMax<float> <= kPartsMax && kPartsMax <= GEM_TOP_MAX,
+              "a row's parts are joined by one block, by the threads that hold entries");
 
 template <class T>
 hipError_t scores(const ScoreArgs& a, const OpsDevice& d, hipStream_t stream)

@@ -120,3 +120,21 @@ def test_distill_gradient_of_records_of_any_mass_against_differences(torch, G, o
         lo[v] -= step
         d = (loss(hi) - loss(lo)) / (2 * step)
         assert abs(d - float(g[0, v])) < 2e-5 * max(abs(d), 0.05), v
+
+
+# ---- the tail -----------------------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(8, 50), (8, 9001), (3, 90001), (280, 3001), (264, 40001), (258, 70001)])
+@pytest.mark.parametrize("gap,T", [(60.0, 1.0), (80.0, 1.0), (90.0, 1.0), (100.0, 1.0), (200.0, 1.0), (10.0, 0.05),
+                                   (600.0, 1.0)])
+def test_distill_tail_far_below_the_listed_tokens(torch, G, rows, V, gap, T, dt):
+    """Unlisted logits so far down that their exponentials, taken about the listed ones, are
+    nothing in 32 bits."""
+    rng = np.random.default_rng(int(gap) + V)
+    ids, lp = _teacher(rng, rows, V, 6)
+    z = rng.normal(size=(rows, V))
+    for r in range(rows):
+        z[r, ids[r, :1 + r % 6]] += gap
+    _check_distill(torch, G, z, ids, lp, dt, T=T, tail=1, what=f"gap {gap}")
+    if rows < 9:
+        _check_distill(torch, G, z, ids, lp, dt, T=T, tail=1, in_place=True, what=f"gap {gap}, in place")

@@ -482,7 +482,8 @@ int gem_token_scores(gem_ops_t* ops, const gem_logits* z, const int32_t* tokens,
  * tail 0: the entries are a distribution of their own (their probabilities are
  * scaled to sum 1).  tail 1: they are part of the teacher's distribution, and
  * what is missing to 1 stands for all tokens that are not listed, as one more
- * outcome. */
+ * outcome.  A NaN among the log probabilities of entries makes the row's loss and
+ * gradient NaN. */
 typedef struct {
     const int32_t* ids;
     const float* logprob;

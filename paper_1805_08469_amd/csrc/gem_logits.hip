@@ -623,7 +623,8 @@ __device__ __forceinline__ int distinct(const Entry& e, int k, DistillLds& l)
 }
 
 // Thread i's entry as it counts: its token (-1: none), log probability and probability; the
-// row's p_t and mass, the sum of all p and p_t; and the token's logit.
+// row's p_t and mass, the sum of all p and p_t; and the token's logit.  A NaN in a record makes
+// its p, the mass and with them loss and gradient NaN.
 struct Teacher {
     int id = -1;
     float lp = 0.0f, p = 0.0f, pt = 0.0f, mass = 0.0f, x = -kInf;
@@ -639,15 +640,15 @@ __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const Entry&
         t.lp = lp;
         t.p = t.id >= 0 ? expf(lp) : 0.0f;
         const float sum = block_sum<WAVES>(t.p, l.red);
-        t.pt = __builtin_fmaxf(0.0f, 1.0f - sum);
-        t.mass = __builtin_fmaxf(1.0f, sum);
+        t.pt = sum > 1.0f ? 0.0f : 1.0f - sum;
+        t.mass = sum <= 1.0f ? 1.0f : sum;
     } else {
         const float top = block_max<WAVES>(lp, l.red);
-        t.p = t.id >= 0 && top > -kInf ? expf(lp - top) : 0.0f;
+        t.p = lp == -kInf ? 0.0f : expf(lp - top);
         const float sum = block_sum<WAVES>(t.p, l.red);
         t.lp = lp - (top + logf(sum));
-        t.p = sum > 0.0f ? t.p / sum : 0.0f;
-        t.mass = sum > 0.0f ? 1.0f : 0.0f;
+        t.p = sum == 0.0f ? 0.0f : t.p / sum;
+        t.mass = sum == 0.0f ? 0.0f : sum / sum;
     }
     return t;
 }
@@ -800,7 +801,7 @@ template <int WAVES>
 __device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t, const RowSums& u, DistillLds& l)
 {
     float part = 0.0f;
-    if (t.p > 0.0f) part = t.p * (t.lp - log_prob(a.l, t.x, u.top, u.ls));
+    if (t.p != 0.0f) part = t.p * (t.lp - log_prob(a.l, t.x, u.top, u.ls));
     float loss = block_sum<WAVES>(part, l.red);
     if (t.pt > 0.0f) loss += u.no_rest(a.l.scale) ? kInf : t.pt * (logf(t.pt) - u.rest(a.l.scale) * kLn2);
     return loss;

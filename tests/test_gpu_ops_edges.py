@@ -122,6 +122,27 @@ def test_distill_gradient_of_records_of_any_mass_against_differences(torch, G, o
         assert abs(d - float(g[0, v])) < 2e-5 * max(abs(d), 0.05), v
 
 
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("rows,V", [(5, 60), (2, 90001), (300, 3001)])
+def test_distill_of_records_with_a_nan_is_nan(torch, G, rows, V, tail):
+    """A broken record shows in its row's loss and gradient, and in no other's."""
+    rng = np.random.default_rng(23)
+    ids, lp = _teacher(rng, rows, V, 5)
+    lp[1, 2] = np.nan
+    z, _ = _matrix(torch, rng.normal(size=(rows, V)), "f32")
+    ti, tl = torch.from_numpy(ids).cuda(), torch.from_numpy(lp).cuda()
+    loss, loss2 = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    g = torch.zeros(rows, V, device="cuda")
+    args = dict(ids=ti.data_ptr(), teacher=tl.data_ptr(), k=5, tail=tail)
+    with G.Ops() as ops:
+        ops.distill_loss(z.data_ptr(), rows, V, 0, loss=loss.data_ptr(), **args)
+        ops.distill_grad(z.data_ptr(), rows, V, 0, loss=loss2.data_ptr(), grad=g.data_ptr(), **args)
+        torch.cuda.synchronize()
+    for out in (loss, loss2, g[:, 0], g[:, V - 1]):
+        assert torch.isnan(out).tolist() == [r == 1 for r in range(rows)]
+    assert bool(torch.isnan(g[1]).all())
+
+
 # ---- the tail -----------------------------------------------------------------------
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,V", [(8, 50), (8, 9001), (3, 90001), (280, 3001), (264, 40001), (258, 70001)])

@@ -496,8 +496,9 @@ typedef struct {
  * of q = softmax(logits / temperature) from the teacher's p; with tail, p_t =
  * max(0, 1 - sum_i p_i) and q_t = sum of q over unlisted tokens (0 where it is
  * below 2^-1022, as for tokens masked by a large finite logit: the loss is then
- * infinite, and the tail has no part in the gradient).  Outcomes with p = 0 add
- * nothing; a row without entries has loss 0.  weight ([rows], NULL:
+ * infinite, and the tail has no part in the gradient; but a p_t of up to 2^-16
+ * counts as 0 there, as the rounding of a record of all tokens that can occur).
+ * Outcomes with p = 0 add nothing; a row without entries has loss 0.  weight ([rows], NULL:
  * all 1) is the factor of the row's loss in what is minimised: it does not
  * multiply loss[r], but a row of weight 0 (padding) has loss 0 and its logits
  * are not read.  Errors: EINVAL, EDTYPE, EALIGN. */

@@ -796,6 +796,16 @@ struct RowSums {
     __device__ bool no_rest(float scale) const { return s == 0.0f || rest(scale) < -1022.0f; }
 };
 
+// A record of all tokens that can occur leaves its rounding for the tail (log probabilities of
+// 32 bits, at most GEM_TOP_MAX of them), which no unlisted token of the student's can answer.
+constexpr float kNoTail = 0x1p-16f;
+__device__ __forceinline__ void drop_tail(Teacher& t, const RowSums& u, float scale)
+{
+    if (!(t.pt > 0.0f && t.pt <= kNoTail && u.no_rest(scale))) return;
+    t.mass -= t.pt;
+    t.pt = 0.0f;
+}
+
 // The row's loss, from thread i's entry.
 template <int WAVES>
 __device__ __forceinline__ float loss_of(const DistillArgs& a, const Teacher& t, const RowSums& u, DistillLds& l)
@@ -960,6 +970,7 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a, 
         sums = block_parts<WAVES>(run, listed, a.tail, scale, l.sums);
     }
     const RowSums u(sums, scale);
+    drop_tail(t, u, scale);
     const float loss = loss_of<WAVES>(a, t, u, l);     // and every entry's logit is read
     if (a.loss && q == 0 && tid == 0) a.loss[r] = loss;
     if (!grad) return;
@@ -1105,6 +1116,7 @@ __global__ __launch_bounds__(THREADS, 4) void resident_kernel(const DistillArgs 
         if (a.tail) listed = listed_of(part, t);
         stores_done();
         const RowSums sums(block_parts<WAVES>(run, listed, a.tail, scale, l.sums), scale);
+        drop_tail(t, sums, scale);
         if (listed_id >= 0) store(listed_grad, listed_id, listed_value);
         const float loss = loss_of<WAVES>(a, t, sums, l);      // and every entry's logit is read
         if (tid == 0 && a.loss) a.loss[r] = loss;

@@ -159,3 +159,29 @@ def test_distill_tail_far_below_the_listed_tokens(torch, G, rows, V, gap, T, dt)
     _check_distill(torch, G, z, ids, lp, dt, T=T, tail=1, what=f"gap {gap}")
     if rows < 9:
         _check_distill(torch, G, z, ids, lp, dt, T=T, tail=1, in_place=True, what=f"gap {gap}, in place")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,possible", [(4, 12, 12), (3, 4000, 20), (2, 90001, 20), (300, 3001, 20)])
+def test_a_record_of_all_possible_tokens_distils_into_itself(torch, G, rows, V, possible, dt):
+    """Where every token that can occur is listed nothing is left for the tail but the record's
+    rounding."""
+    rng = np.random.default_rng(24)
+    k = 24
+    values = np.full((rows, V), -INF)
+    for r in range(rows):
+        values[r, rng.permutation(V)[:possible]] = rng.normal(size=possible) * 3
+    z, _ = _matrix(torch, values, dt)
+    ids = torch.zeros(rows, k, device="cuda", dtype=torch.int32)
+    lp, loss = torch.zeros(rows, k, device="cuda"), torch.zeros(rows, device="cuda")
+    g = torch.zeros(rows, V, device="cuda", dtype=z.dtype)
+    with G.Ops() as ops:
+        for T in (1.0, 0.7, 1.9):
+            ops.token_scores(z.data_ptr(), rows, V, DT[dt], temperature=T, top_k=k, top_ids=ids.data_ptr(),
+                             top_logprob=lp.data_ptr())
+            ops.distill_grad(z.data_ptr(), rows, V, DT[dt], temperature=T, ids=ids.data_ptr(), teacher=lp.data_ptr(), k=k,
+                             tail=1, loss=loss.data_ptr(), grad=g.data_ptr())
+            torch.cuda.synchronize()
+            # both sides carry the bounds of their log probabilities (of at most 30 nats)
+            tol = 4 * R.U * (V / 256 + 64 + 4 * 30)
+            assert float(loss.abs().max()) < tol and float(g.float().abs().max()) < tol / T

@@ -192,8 +192,9 @@ template <class T> struct Part {
     }
 };
 
-// The largest that is a number.  (Written out: for a maximum of bits that might be a
-// signalling NaN the compiler quiets them first.)
+// The largest that is a number, but NaN after a signalling NaN.  (Written out: for a maximum of
+// bits that might be one the compiler quiets them first.)  A sum over the same elements is NaN
+// then.
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float m;
@@ -349,6 +350,38 @@ __device__ uint64_t bound_of(TopLds& l, int mine, int k, int fit, F key)
         }
     }
     return bound ? bound : 1;
+}
+
+// The keys once more, for a part with a NaN: a signalling one may have hidden the numbers beside
+// it from max3, and to a comparison all are alike.  Each key is written by the thread that wrote
+// it before.
+template <class T>
+__device__ void key_again(const Part<T>& part, typename GroupKey<T>::Type* keys, int groups, float& high)
+{
+    constexpr int kLanes = kGroup / kVec<T>;
+    const int tid = threadIdx.x;
+    const auto most = [](const float (&x)[kVec<T>], float m) {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) m = x[i] > m ? x[i] : m;
+        return m;
+    };
+    float x[kVec<T>];
+    high = -kInf;
+    if (tid < 2) {
+        part.edge(x);
+        high = most(x, high);
+        keys[tid == 0 ? 0 : groups - 1] = GroupKey<T>::of(high);
+    }
+    if (tid % kLanes) return;
+    for (int g = tid / kLanes; g < groups - 2; g += kThreads / kLanes) {
+        float m = -kInf;
+        for (int v = g * kLanes; v < (g + 1) * kLanes && v < part.nvec; ++v) {
+            unpack(part.body()[v], x);
+            m = most(x, m);
+        }
+        keys[1 + g] = GroupKey<T>::of(m);
+        high = m > high ? m : high;
+    }
 }
 
 // The part's k largest logits as keys in l.sel (0 where there are fewer).  keys holds
@@ -521,8 +554,13 @@ __global__ __launch_bounds__(kThreads) void score_kernel(const ScoreArgs a, int6
         }
     });
     const Sums u = block_sums<kThreads / 64>(run, scale, lds);
-    if constexpr (TOP)
+    if constexpr (TOP) {
+        if (__builtin_expect(u.s != u.s, 0)) {
+            key_again(part, keys, groups, high);
+            seen = high;
+        }
         select_top(top, part, keys, groups, order(high) >> shift, order(kVec<T> < kGroup ? seen : high) >> shift, a.top_k);
+    }
     if (parts == 1) {
         write_scores(a, r, row, u, top.sel);
     } else {

@@ -185,3 +185,32 @@ def test_a_record_of_all_possible_tokens_distils_into_itself(torch, G, rows, V, 
             # both sides carry the bounds of their log probabilities (of at most 30 nats)
             tol = 4 * R.U * (V / 256 + 64 + 4 * 30)
             assert float(loss.abs().max()) < tol and float(g.float().abs().max()) < tol / T
+
+
+# ---- scores --------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(6, 9), (6, 700), (6, 20001), (2, 90001)])
+def test_scores_alternatives_beside_a_signalling_nan(torch, G, rows, V, dt):
+    """Every NaN is left out of the alternatives, whatever its bits."""
+    rng = np.random.default_rng(26)
+    z = rng.normal(size=(rows, V)) * 3
+    z, buf = _matrix(torch, z, dt)
+    bits = z.view(torch.int32 if dt == "f32" else torch.int16)
+    codes = (0x7FA00001, -0x005FFFFF) if dt == "f32" else (0x7FA1, -0x005F)
+    best = z.float().argsort(dim=1, descending=True)[:, :4].cpu().numpy()
+    for r in range(rows):
+        for i, b in enumerate(best[r]):
+            # beside the row's largest, on one side or the other
+            at = min(V - 1, b + 1) if (r + i) % 2 else max(0, b - 1)
+            if at not in best[r]:
+                bits[r, int(at)] = codes[i % 2]
+    with np.errstate(invalid="ignore"):
+        host = z.float().cpu().numpy().astype(np.float64)
+    broken = np.isnan(host).any(axis=1)
+    assert broken.any()
+    k = min(8, V)
+    got = _score(torch, G, z, 1.0, None, k, dt)
+    want = R.scores(host, 1.0, np.zeros((rows, 0), int), k)
+    assert np.array_equal(got["top_ids"].cpu().numpy(), want["top_ids"])
+    for name in ("lse", "entropy"):
+        assert np.array_equal(np.isnan(_host(got[name])), broken)

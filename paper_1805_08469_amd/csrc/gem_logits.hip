@@ -478,6 +478,11 @@ __device__ __forceinline__ float log_prob(const LogitArgs& a, float x, float ref
     return x == -kInf ? x : (x - ref) * a.inv_t - ls * kLn2;
 }
 
+// A log probability and an entropy have a side of 0 to be on, which near a single outcome is
+// less than their rounding.
+__device__ __forceinline__ float at_most_0(float v) { return v > 0.0f ? 0.0f : v; }
+__device__ __forceinline__ float at_least_0(float v) { return v < 0.0f ? 0.0f : v; }
+
 // A row's outputs from its sums and its alternatives' keys.
 template <class T>
 __device__ void write_scores(const ScoreArgs& a, int64_t r, const T* row, const Sums& u, const uint64_t* top)
@@ -485,12 +490,12 @@ __device__ void write_scores(const ScoreArgs& a, int64_t r, const T* row, const 
     const float ls = __builtin_log2f(u.s);
     if (threadIdx.x == 0) {
         if (a.out.lse) a.out.lse[r] = u.ref * a.l.inv_t + ls * kLn2;
-        if (a.out.entropy) a.out.entropy[r] = u.s == 0.0f ? 0.0f : (ls - u.t / u.s) * kLn2;
+        if (a.out.entropy) a.out.entropy[r] = u.s == 0.0f ? 0.0f : at_least_0((ls - u.t / u.s) * kLn2);
     }
     for (int i = threadIdx.x; i < a.n_tokens; i += kThreads) {
         const int token = a.tokens[r * a.n_tokens + i];
         float lp = 0.0f;
-        if (token >= 0 && token < a.l.vocab) lp = log_prob(a.l, load(row, token), u.ref, ls);
+        if (token >= 0 && token < a.l.vocab) lp = at_most_0(log_prob(a.l, load(row, token), u.ref, ls));
         a.out.logprob[r * a.n_tokens + i] = lp;
     }
     for (int i = threadIdx.x; i < a.top_k; i += kThreads) {
@@ -498,7 +503,7 @@ __device__ void write_scores(const ScoreArgs& a, int64_t r, const T* row, const 
         if (a.out.top_ids) a.out.top_ids[r * a.top_k + i] = key ? key_token(key) : -1;
         if (a.out.top_logprob)
             a.out.top_logprob[r * a.top_k + i] =
-                key ? log_prob(a.l, ordered(static_cast<uint32_t>(key >> 32)), u.ref, ls) : -kInf;
+                key ? at_most_0(log_prob(a.l, ordered(static_cast<uint32_t>(key >> 32)), u.ref, ls)) : -kInf;
     }
 }
 

@@ -189,6 +189,20 @@ def test_a_record_of_all_possible_tokens_distils_into_itself(torch, G, rows, V, 
 
 # ---- scores --------------------------------------------------------------------------
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(64, 30), (64, 3001), (2, 90001)])
+def test_scores_are_those_of_probabilities(torch, G, rows, V, dt):
+    """Near a single outcome: no probability above 1, no entropy below 0."""
+    rng = np.random.default_rng(25)
+    z = rng.normal(size=(rows, V)) * 0.3
+    z[np.arange(rows), rng.integers(0, V, rows)] += rng.uniform(2, 40, rows) + math.log(V)
+    z += rng.normal(size=(rows, 1)) * 5
+    zt, _ = _matrix(torch, z, dt)
+    for T in (1.0, 0.9, 0.37):
+        got = _score(torch, G, zt, T, None, 3, dt)
+        assert float(got["top_logprob"].max()) <= 0 and float(got["entropy"].min()) >= 0
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,V", [(6, 9), (6, 700), (6, 20001), (2, 90001)])
 def test_scores_alternatives_beside_a_signalling_nan(torch, G, rows, V, dt):
     """Every NaN is left out of the alternatives, whatever its bits."""

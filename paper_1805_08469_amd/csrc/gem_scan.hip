@@ -622,6 +622,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(const ScanArgs a, int sl
         const Raw<T> rx = fetch<T, KIND>(static_cast<const T*>(a.s.x) + t * a.s.x_stride, o);
         const Raw<T> rg = fetch<T, KIND>(static_cast<const T*>(a.s.gate) + t * a.s.gate_stride, o);
         fetch_or_zero(a.s.h0, t, o, h);
+        if (a.states && t % kStateTokens == 0) put_f32(a.states + t / kStateTokens * D, o, h);
         widen(rx[0], rx[1], x);
         widen(rg[0], rg[1], g);
 #pragma unroll

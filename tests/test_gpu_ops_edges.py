@@ -228,3 +228,33 @@ def test_scores_alternatives_beside_a_signalling_nan(torch, G, rows, V, dt):
     assert np.array_equal(got["top_ids"].cpu().numpy(), want["top_ids"])
     for name in ("lse", "entropy"):
         assert np.array_equal(np.isnan(_host(got[name])), broken)
+
+
+# ---- the recurrence -------------------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("B,D", [(1, 3), (8, 64), (21, 137), (64, 520)])
+def test_single_tokens_leave_their_states(torch, G, B, D, dt):
+    """A training call of one token a sequence keeps its states as any other does."""
+    rng = np.random.default_rng(27)
+    x, _ = _matrix(torch, rng.normal(size=(B, D)), dt)
+    g, _ = _matrix(torch, rng.normal(size=(B, D)), dt)
+    h0 = torch.from_numpy(rng.normal(size=(B, D)).astype(np.float32)).cuda()
+    rows = G.gem_scan_state_rows(B)
+    states = torch.full((rows * D + 4,), math.nan, device="cuda")
+    y, dx, dg = (torch.zeros(B, D, device="cuda", dtype=x.dtype) for _ in range(3))
+    d0 = torch.zeros(B, D, device="cuda")
+    dy, _ = _matrix(torch, rng.normal(size=(B, D)), dt)
+    args = (x.data_ptr(), g.data_ptr(), B, D, B, DT[dt])
+    with G.Ops(G.gem_scan_scratch(B, D)) as ops:
+        ops.scan_forward(*args, y=y.data_ptr(), h0=h0.data_ptr(), states=states.data_ptr())
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(states[:rows * D]).all()) and bool(torch.isnan(states[rows * D:]).all())
+        ops.scan_backward(*args, h0=h0.data_ptr(), states=states.data_ptr(), dy=dy.data_ptr(), dx=dx.data_ptr(),
+                          dgate=dg.data_ptr(), dh0=d0.data_ptr())
+        torch.cuda.synchronize()
+    u = R.BF16_U if dt == "bf16" else 0.0
+    for b in range(B):
+        w = R.scan(_host(x)[b:b + 1], _host(g)[b:b + 1], _host(h0)[b], _host(dy)[b:b + 1], np.zeros(D))
+        _same(_host(dx)[b:b + 1], w["dx"], w["dxe"] + u * np.abs(w["dx"]) + 1e-37, "dx")
+        _same(_host(dg)[b:b + 1], w["dg"], w["dge"] + u * np.abs(w["dg"]) + 1e-37, "dgate")
+        _same(_host(d0)[b], w["dh0"], w["dh0e"] + 1e-37, "dh0")

@@ -540,9 +540,9 @@ typedef struct {
     int32_t reserved;
 } gem_scan;
 
-/* Scratch bytes that a gem_ops_t needs for recurrences of these sizes (the same
- * for both directions), and the rows of the states that forward keeps for
- * backward. */
+/* Scratch bytes that a gem_ops_t needs for recurrences of up to these sizes (the
+ * same for both directions; fewer tokens or channels never need more), and the
+ * rows of the states that forward keeps for backward. */
 int gem_scan_scratch(int64_t tokens, int32_t channels, int64_t* bytes);
 int gem_scan_state_rows(int64_t tokens, int64_t* rows);
 

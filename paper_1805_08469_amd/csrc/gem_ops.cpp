@@ -222,7 +222,7 @@ int gem_scan_forward(gem_ops_t* ops, const gem_scan* s, void* y, int64_t y_strid
     a.y = y;
     a.h_last = h_last;
     a.states = states;
-    if (gemk::scan_scratch_bytes(s->tokens, s->channels) > ops->dev.scan_bytes && !single_tokens(*s))
+    if (gemk::scan_bytes(s->tokens, s->channels) > ops->dev.scan_bytes && !single_tokens(*s))
         return GEM_ESCRATCH;
     OPS_HIP(gemk::launch_scan_forward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
@@ -249,7 +249,7 @@ int gem_scan_backward(gem_ops_t* ops, const gem_scan* s, const float* states, co
     a.dx = dx;
     a.dgate = dgate;
     a.dh0 = dh0;
-    if (gemk::scan_scratch_bytes(s->tokens, s->channels) > ops->dev.scan_bytes) return GEM_ESCRATCH;
+    if (gemk::scan_bytes(s->tokens, s->channels) > ops->dev.scan_bytes) return GEM_ESCRATCH;
     OPS_HIP(gemk::launch_scan_backward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
 }

@@ -80,7 +80,8 @@ struct OpsDevice {
 hipError_t launch_scores(const ScoreArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_distill(const DistillArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 int64_t scan_rows(int64_t tokens, int64_t channels);
-int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);
+int64_t scan_bytes(int64_t tokens, int64_t channels);            // of a launch
+int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);    // of it and of any smaller one
 hipError_t launch_scan_forward(const ScanArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_scan_backward(const ScanBackArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 

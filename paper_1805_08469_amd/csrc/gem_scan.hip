@@ -669,13 +669,14 @@ hipError_t pass_all(const gem_scan& s, const float* from, float* to, hipStream_t
 // 16384 x 2048 93 / 88 / 90 (2048, 4096 and 8192 rows); both directions of 8192 x 4096 are 189
 // with 2048 rows, 200 with 4096.
 constexpr int64_t kForwardRows = 4096, kBackwardRows = 2048;
+constexpr int kRunMost = 128, kRunLeast = 16;
 int run_len(int64_t tokens, int64_t slices, int64_t least)
 {
-    int len = 128;
-    while (len > 16 && over(tokens, len) * slices < least) len /= 2;
+    int len = kRunMost;
+    while (len > kRunLeast && over(tokens, len) * slices < least) len /= 2;
     return len;
 }
-static_assert(16 % kStateTokens == 0, "runs begin where states are kept");
+static_assert(kRunLeast % kStateTokens == 0, "runs begin where states are kept");
 
 template <class T> Runs runs_of(const gem_scan& s, const OpsDevice& d, int64_t least)
 {
@@ -762,11 +763,27 @@ int64_t scan_rows(int64_t tokens, int64_t channels)
     return over(tokens, run_len(tokens, slices, kForwardRows)) * slices;
 }
 
+// A run's A, B and state, of each channel.
+constexpr int64_t kRunBytes = 3 * static_cast<int64_t>(sizeof(float));
+
 // For the most runs: of the type with the wider slices, in the direction with the shorter runs.
-int64_t scan_scratch_bytes(int64_t tokens, int64_t channels)
+int64_t scan_bytes(int64_t tokens, int64_t channels)
 {
     const int64_t runs = over(tokens, run_len(tokens, over(channels, kSlice<uint16_t>), kForwardRows));
-    return runs <= 1 ? 0 : runs * channels * 3 * static_cast<int64_t>(sizeof(float));
+    return runs <= 1 ? 0 : runs * channels * kRunBytes;
+}
+
+// Enough for these sizes and all smaller ones.  Fewer tokens can have more runs, since those get
+// shorter where the rows would be too few; but with runs of less than 128 tokens twice as long
+// ones would leave less than kForwardRows rows, so that the runs' channels are fewer than those of
+// 2 kForwardRows slices.
+int64_t scan_scratch_bytes(int64_t tokens, int64_t channels)
+{
+    if (tokens <= kRunLeast) return 0;
+    const int64_t longest = over(tokens, kRunMost) * channels, shortest = over(tokens, kRunLeast) * channels;
+    const int64_t most = 2 * kForwardRows * kSlice<uint16_t>;
+    const int64_t capped = shortest < most ? shortest : most;
+    return (longest > capped ? longest : capped) * kRunBytes;
 }
 
 hipError_t launch_scan_forward(const ScanArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream)

@@ -258,3 +258,14 @@ def test_single_tokens_leave_their_states(torch, G, B, D, dt):
         _same(_host(dx)[b:b + 1], w["dx"], w["dxe"] + u * np.abs(w["dx"]) + 1e-37, "dx")
         _same(_host(dg)[b:b + 1], w["dg"], w["dge"] + u * np.abs(w["dg"]) + 1e-37, "dgate")
         _same(_host(d0)[b], w["dh0"], w["dh0e"] + 1e-37, "dh0")
+
+
+@pytest.mark.parametrize("most,tokens,channels", [(32768, 32640, 2048), (4097, 4096, 130), (70000, 65535, 513)])
+def test_a_handle_for_the_longest_batch_takes_shorter_ones(torch, G, most, tokens, channels):
+    x = torch.randn(tokens, channels, device="cuda", dtype=torch.bfloat16)
+    y, y2 = torch.zeros_like(x), torch.zeros_like(x)
+    with G.Ops(G.gem_scan_scratch(most, channels)) as ops, G.Ops(G.gem_scan_scratch(tokens, channels)) as own:
+        ops.scan_forward(x.data_ptr(), x.data_ptr(), tokens, channels, 1, G.GEM_BF16, y=y.data_ptr())
+        own.scan_forward(x.data_ptr(), x.data_ptr(), tokens, channels, 1, G.GEM_BF16, y=y2.data_ptr())
+        torch.cuda.synchronize()
+    assert torch.equal(y, y2)

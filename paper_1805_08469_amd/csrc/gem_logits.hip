@@ -770,27 +770,37 @@ __device__ __forceinline__ float moved(float t, float ref, float to, float scale
     return t == 0.0f ? 0.0f : t * __builtin_amdgcn_exp2f((ref - to) * scale);
 }
 
+template <int CTRL> __device__ __forceinline__ float other_lane(float v)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true));
+}
+// Two values joined over the wave, step by step together, the steps inside a row of 16 lanes
+// without LDS: with the second value's reductions a small call would take 0.3 to 0.6 us longer.
+template <class F> __device__ __forceinline__ void wave_both(float& a, float& b, F f)
+{
+    const auto step = [&](auto get) {
+        const float x = get(a), y = get(b);
+        a = f(a, x);
+        b = f(b, y);
+    };
+    step([](float v) { return other_lane<0xB1>(v); });         // its neighbour in a pair
+    step([](float v) { return other_lane<0x4E>(v); });         // the other pair of four
+    step([](float v) { return other_lane<0x141>(v); });        // the other four of eight
+    step([](float v) { return other_lane<0x140>(v); });        // the other eight of sixteen
+    step([](float v) { return __shfl_xor(v, 16); });
+    step([](float v) { return __shfl_xor(v, 32); });
+}
+
 // A row's (or a part's) sums: s of unlisted tokens (without a tail of all) about ref, t of listed
 // ones about lref; a reference is -inf where no logit is above it.
 template <int WAVES>
 __device__ __forceinline__ PartSums block_parts(const Run& r, Listed l, bool tail, float scale, float (*lds)[4])
 {
-    // Both halves step by step together: a step of one covers the wait for the other's.
     float top = r.at.ref, ltop = l.ref;
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) {
-        const float a = __shfl_xor(top, m), b = __shfl_xor(ltop, m);
-        top = __builtin_fmaxf(top, a);
-        ltop = __builtin_fmaxf(ltop, b);
-    }
+    wave_both(top, ltop, [](float a, float b) { return __builtin_fmaxf(a, b); });
     float s = r.s, none = 0.0f, t = moved(l.t, l.ref, ltop, scale);
     if (r.at.ref > -kInf) shift_sums<false>(s, none, (r.at.ref - top) * scale - r.at.skew(scale));
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) {
-        const float a = __shfl_xor(s, m), b = __shfl_xor(t, m);
-        s += a;
-        t += b;
-    }
+    wave_both(s, t, [](float a, float b) { return a + b; });
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) {
         lds[wave][0] = top;

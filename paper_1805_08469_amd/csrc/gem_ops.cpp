@@ -8,7 +8,6 @@
 #include "gem_ops.hpp"
 
 struct gem_ops_handle {
-    int device = 0;
     hipStream_t stream = nullptr;
     void* memory = nullptr;
     gemk::OpsDevice dev{};
@@ -99,8 +98,9 @@ int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out)
     if (!o) return GEM_ENOMEM;
     o->stream = static_cast<hipStream_t>(stream);
     const int rc = [&]() -> int {
-        OPS_HIP(hipGetDevice(&o->device));
-        OPS_HIP(hipDeviceGetAttribute(&o->dev.cus, hipDeviceAttributeMultiprocessorCount, o->device));
+        int device = 0;
+        OPS_HIP(hipGetDevice(&device));
+        OPS_HIP(hipDeviceGetAttribute(&o->dev.cus, hipDeviceAttributeMultiprocessorCount, device));
         if (scratch_bytes > INT64_MAX - gemk::kFixedScratch) return GEM_ENOMEM;
         const size_t bytes = static_cast<size_t>(scratch_bytes + gemk::kFixedScratch);
         const hipError_t e = hipMalloc(&o->memory, bytes);

@@ -161,6 +161,36 @@ def test_distill_tail_far_below_the_listed_tokens(torch, G, rows, V, gap, T, dt)
         _check_distill(torch, G, z, ids, lp, dt, T=T, tail=1, in_place=True, what=f"gap {gap}, in place")
 
 
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(12, 60), (12, 9001), (4, 90001), (1300, 3001), (520, 40001), (520, 70001)])
+def test_distill_of_logits_that_are_no_numbers(torch, G, rows, V, dt, tail):
+    """NaN and +inf, listed or not: NaN in the row's loss and all of its gradient, and nothing in
+    any other row, the next one of the same block among them."""
+    rng = np.random.default_rng(28)
+    ids, lp = _teacher(rng, rows, V, 6)
+    z = torch.randn(rows, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(28)).to(
+        torch.float32 if dt == "f32" else torch.bfloat16)
+    bad = np.arange(1, rows, 3)
+    for r in bad:
+        other = next(v for v in rng.permutation(V) if v not in ids[r])
+        z[r, int(ids[r, 2] if r % 2 else other)] = math.nan if r % 4 < 2 else INF
+    ti, tl = torch.from_numpy(ids).cuda(), torch.from_numpy(lp).cuda()
+    loss, loss2 = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    g = torch.zeros_like(z)
+    args = dict(ids=ti.data_ptr(), teacher=tl.data_ptr(), k=6, tail=tail)
+    with G.Ops() as ops:
+        ops.distill_loss(z.data_ptr(), rows, V, DT[dt], loss=loss.data_ptr(), **args)
+        ops.distill_grad(z.data_ptr(), rows, V, DT[dt], loss=loss2.data_ptr(), grad=g.data_ptr(), **args)
+        torch.cuda.synchronize()
+    want = np.zeros(rows, bool)
+    want[bad] = True
+    for out in (loss, loss2, g.float().sum(1)):
+        assert np.array_equal(np.isnan(_host(out)), want)
+    assert bool(torch.isnan(g[torch.from_numpy(bad).cuda()]).all())
+    assert bool(torch.isfinite(g[torch.from_numpy(~want).cuda()]).all())
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,V,possible", [(4, 12, 12), (3, 4000, 20), (2, 90001, 20), (300, 3001, 20)])
 def test_a_record_of_all_possible_tokens_distils_into_itself(torch, G, rows, V, possible, dt):
@@ -269,3 +299,43 @@ def test_a_handle_for_the_longest_batch_takes_shorter_ones(torch, G, most, token
         own.scan_forward(x.data_ptr(), x.data_ptr(), tokens, channels, 1, G.GEM_BF16, y=y2.data_ptr())
         torch.cuda.synchronize()
     assert torch.equal(y, y2)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_nothing_passes_from_one_sequence_to_another(torch, G, dt):
+    """NaN and infinities in one sequence of a pack, in both directions."""
+    lengths, D = [300, 40, 700, 5, 333], 72
+    off = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int64)
+    N, B = int(off[-1]), len(lengths)
+    rng = np.random.default_rng(29)
+    x, g, dy = (_matrix(torch, rng.normal(size=(N, D)) + m, dt)[0] for m in (0, 2, 0))
+    h0, dl = (torch.from_numpy(rng.normal(size=(B, D)).astype(np.float32)).cuda() for _ in range(2))
+    offs = torch.from_numpy(off).cuda()
+
+    def go():
+        y, dx, dg = (torch.zeros_like(x) for _ in range(3))
+        last, d0 = torch.zeros_like(h0), torch.zeros_like(h0)
+        states = torch.zeros(G.gem_scan_state_rows(N), D, device="cuda")
+        args = dict(x=x.data_ptr(), gate=g.data_ptr(), tokens=N, channels=D, sequences=B, dtype=DT[dt], offsets=offs.data_ptr(),
+                    h0=h0.data_ptr())
+        with G.Ops(G.gem_scan_scratch(N, D)) as ops:
+            ops.scan_forward(y=y.data_ptr(), h_last=last.data_ptr(), states=states.data_ptr(), **args)
+            ops.scan_backward(states=states.data_ptr(), dy=dy.data_ptr(), dx=dx.data_ptr(), dgate=dg.data_ptr(),
+                              dh_last=dl.data_ptr(), dh0=d0.data_ptr(), **args)
+            torch.cuda.synchronize()
+        return (y, dx, dg), (last, d0)
+
+    whole, ends = go()
+    for broken in (1, 2, 4):
+        for value in (math.nan, INF):
+            kept = [a.clone() for a in (x, dy, h0, dl)]
+            lo, hi = int(off[broken]), int(off[broken + 1])
+            x[lo:hi:7], dy[lo:hi:5], h0[broken], dl[broken] = value, value, value, value
+            rows, rest = go()
+            for a, b in zip(kept, (x, dy, h0, dl)):
+                b.copy_(a)
+            for a, b in zip(rows, whole):
+                assert torch.equal(a[:lo], b[:lo]) and torch.equal(a[hi:], b[hi:])
+                assert not bool(torch.isfinite(a[hi - 1]).any())
+            for a, b in zip(rest, ends):
+                assert torch.equal(a[:broken], b[:broken]) and torch.equal(a[broken + 1:], b[broken + 1:])

@@ -1,5 +1,5 @@
 """The worker's operators at the sizes that take their other paths: more rows of logits than
-blocks, runs of every length, more rows than one launch takes."""
+blocks, runs of every length, more rows than one launch takes, more elements than 32 bits count."""
 import numpy as np
 import pytest
 
@@ -122,3 +122,53 @@ def test_scan_in_runs_of_every_length(torch, G, D, lengths, ragged, dt):
         _same(DX[lo:hi], w["dx"], w["dxe"] + u * np.abs(w["dx"]) + 1e-37, f"dx of {b}")
         _same(DG[lo:hi], w["dg"], w["dge"] + u * np.abs(w["dg"]) + 1e-37, f"dgate of {b}")
         _same(D0[b], w["dh0"], w["dh0e"] + 1e-37, f"dh0 of {b}")
+
+
+# ---- offsets past 32 bits --------------------------------------------------------------------
+def test_scores_and_gradients_of_more_elements_than_32_bits_count(torch, G):
+    rows, V, k = 69000, 32768, 8
+    z = torch.randn(rows, V, device="cuda", dtype=torch.bfloat16, generator=torch.Generator(device="cuda").manual_seed(3))
+    ids, top = torch.zeros(rows, k, device="cuda", dtype=torch.int32), torch.zeros(rows, k, device="cuda")
+    loss = torch.zeros(rows, device="cuda")
+    some = np.array([0, 1, 32767, 32768, 65534, 65535, 65536, rows - 2, rows - 1])
+    before = _host(z[some])
+    with G.Ops() as ops:
+        ops.token_scores(z.data_ptr(), rows, V, 1, top_k=k, top_ids=ids.data_ptr(), top_logprob=top.data_ptr(), temperature=0.5)
+        ops.distill_grad(z.data_ptr(), rows, V, 1, ids=ids.data_ptr(), teacher=top.data_ptr(), k=k, tail=1,
+                         loss=loss.data_ptr(), grad=z.data_ptr())
+        torch.cuda.synchronize()
+    want = R.scores(before, 0.5, np.zeros((some.size, 0), int), k)
+    at, lp = ids[some].cpu().numpy(), top[some].cpu().numpy()
+    assert np.array_equal(at, want["top_ids"])
+    _same(lp, want["top_logprob"], R.score_tolerance(V, want["top_logprob"]), "top_logprob")
+    got, grad = _host(loss[some]), _host(z[some])
+    for i in range(some.size):
+        lo, gr, q, p, pt, qt = R.distill_row(before[i], 1.0, at[i], lp[i], 1)
+        lt, gt = R.distill_tolerance(V, k, 1.0, before[i], q, p, pt, qt, lo, gr, 1.0, True)
+        _same(got[i:i + 1], np.array([lo]), lt, f"loss of row {some[i]}")
+        _same(grad[i], gr, gt, f"gradient of row {some[i]}")
+
+
+def test_scan_of_more_elements_than_32_bits_count(torch, G):
+    B, T, D = 1080, 1000, 2048
+    N = B * T
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, g, dy = (torch.randn(N, D, device="cuda", dtype=torch.bfloat16, generator=gen) for _ in range(3))
+    y, dx, dg = (torch.zeros_like(x) for _ in range(3))
+    h0, dl = (torch.randn(B, D, device="cuda", generator=gen) for _ in range(2))
+    last, d0 = torch.zeros_like(h0), torch.zeros_like(h0)
+    states = torch.zeros(G.gem_scan_state_rows(N), D, device="cuda")
+    args = (x.data_ptr(), g.data_ptr(), N, D, B, 1)
+    with G.Ops(G.gem_scan_scratch(N, D)) as ops:
+        ops.scan_forward(*args, y=y.data_ptr(), h0=h0.data_ptr(), h_last=last.data_ptr(), states=states.data_ptr())
+        ops.scan_backward(*args, h0=h0.data_ptr(), states=states.data_ptr(), dy=dy.data_ptr(), dx=dx.data_ptr(),
+                          dgate=dg.data_ptr(), dh_last=dl.data_ptr(), dh0=d0.data_ptr())
+        torch.cuda.synchronize()
+    for b in (0, 524, 1048, 1049, B - 1):          # 2^31 elements end in sequence 1048
+        at = slice(b * T, (b + 1) * T)
+        w = R.scan(_host(x[at]), _host(g[at]), _host(h0[b]), _host(dy[at]), _host(dl[b]))
+        _same(_host(y[at]), w["y"], w["yerr"] + R.BF16_U * np.abs(w["y"]), f"y of sequence {b}")
+        _same(_host(last[b]), w["h_last"], w["h_err"], f"h_last of {b}")
+        _same(_host(dx[at]), w["dx"], w["dxe"] + R.BF16_U * np.abs(w["dx"]) + 1e-37, f"dx of {b}")
+        _same(_host(dg[at]), w["dg"], w["dge"] + R.BF16_U * np.abs(w["dg"]) + 1e-37, f"dgate of {b}")
+        _same(_host(d0[b]), w["dh0"], w["dh0e"] + 1e-37, f"dh0 of {b}")

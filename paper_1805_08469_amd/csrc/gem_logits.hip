@@ -775,7 +775,8 @@ template <int CTRL> __device__ __forceinline__ float other_lane(float v)
     return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true));
 }
 // Two values joined over the wave, step by step together, the steps inside a row of 16 lanes
-// without LDS: with the second value's reductions a small call would take 0.3 to 0.6 us longer.
+// without LDS: a small call takes 0.2 to 0.8 us less than with all of them there (2 x 2280 and 1 x
+// 8753 binary32).
 template <class F> __device__ __forceinline__ void wave_both(float& a, float& b, F f)
 {
     const auto step = [&](auto get) {
@@ -1272,11 +1273,12 @@ void resident(const DistillArgs& a, const OpsDevice& d, hipStream_t stream)
 
 // If there are rows enough to keep the device busy: false where it is not for these sizes.
 // Small blocks, as many on a compute unit as its registers hold, stream while others sum:
-// 4096 rows of 32768 bfloat16 take 119 us in blocks of 256 threads x 16 vectors, 134 in 512 x
-// 8, 197 in 1024 x 4; 4096 of 131072 496 us in 512 x 16 with half of a row read twice, 523 in
-// 1024 x 8, and 621 in 1024 x 16, which read all of it once.  Rows beyond 1024 x 16 vectors
-// are read twice as they are split in parts (1200 of 200000 bfloat16 260 us; 265 here with
-// 1024 x 16 kept).
+// 4096 rows of 32768 bfloat16, all with a weight, take 122 us in blocks of 256 threads x 16
+// vectors, 137 in 512 x 8, 201 in 1024 x 4; 4096 of 131072 525 us in 512 x 16 with half of a row
+// read twice, 562 in 1024 x 8, and 592 in 1024 x 16, which read all of it once.  Rows beyond 1024
+// x 16 vectors are read twice as they are split in parts: 1200 of 200000 284 us; 273 here with
+// 1024 x 16 kept, by a kernel of its own for 4%.  512 x 16 vectors are more than the registers
+// hold: of bfloat16 4 of them spill, and 37 where a row has more.
 template <class T> bool resident_grad(const DistillArgs& a, const OpsDevice& d, hipStream_t stream)
 {
     const int nvec = a.l.vocab / kVec<T>;

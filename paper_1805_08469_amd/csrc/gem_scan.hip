@@ -663,11 +663,11 @@ hipError_t pass_all(const gem_scan& s, const float* from, float* to, hipStream_t
 // Tokens of a run: the most, up to 128, that leave the launches `least` rows of 32 lanes (eight
 // to a compute unit at 2048).  Longer runs have fewer maps to write, join and read; fewer rows
 // leave compute units idle.  us, by runs of 128 / 64 / 32: 32768 x 2048 bfloat16, both
-// directions, 337 / 347 / 379; 65536 x 512 binary32 324 / 343 / 360; 16384 x 512 bfloat16 in
-// two sequences 150 / 102 / 83 (512, 1024 and 2048 rows).  Forward, packed sequences are
+// directions, 336 / 346 / 378; 65536 x 512 binary32 315 / 333 / 347; 16384 x 512 bfloat16 in
+// two sequences 151 / 103 / 85 (512, 1024 and 2048 rows).  Forward, packed sequences are
 // better with twice the rows, since a row in which they begin is walked token by token: 24 of
-// 16384 x 2048 93 / 88 / 90 (2048, 4096 and 8192 rows); both directions of 8192 x 4096 are 189
-// with 2048 rows, 200 with 4096.
+// 16384 x 2048 98 / 92 / 92 (2048, 4096 and 8192 rows); both directions of 8192 x 4096 are 188
+// with 2048 rows, 205 with 4096, and 193 as it is.
 constexpr int64_t kForwardRows = 4096, kBackwardRows = 2048;
 constexpr int kRunMost = 128, kRunLeast = 16;
 int run_len(int64_t tokens, int64_t slices, int64_t least)

@@ -405,8 +405,9 @@ int gem_copy_f32(const float* src, float* dst, int64_t count, void* stream);
  *
  * What a worker computes from data before it has an update to commit: the
  * scores of a model's logits (a teacher's record, an evaluation), the
- * distillation loss against such a record with its gradient, and a gated
- * linear recurrence with its backward pass.  Unlike the commits, which are
+ * distillation loss against such a record and the clipped loss of a policy,
+ * each with its gradient, and a gated linear recurrence with its backward
+ * pass.  Unlike the commits, which are
  * held to fixed bits, their values are those of the formulas up to rounding:
  * inputs are binary32 or bfloat16 (GEM_F32, GEM_BF16), sums, states and
  * statistics are binary32, and outputs of the inputs' type are rounded once
@@ -516,6 +517,56 @@ int gem_distill_loss(gem_ops_t* ops, const gem_logits* z, const gem_teacher* tea
  * loss +inf and q = 0 in its gradient.  Errors: EINVAL, EDTYPE, EALIGN. */
 int gem_distill_grad(gem_ops_t* ops, const gem_logits* z, const gem_teacher* teacher,
                      const float* weight, float* loss, void* grad, int64_t grad_stride);
+
+/* The tokens that a policy took, and what is known of them ([rows] each):
+ * old_logprob under the policy that acted (a worker's older snapshot),
+ * advantage, and ref_logprob under the policy that the KL term holds on to
+ * (NULL: no KL term).  Ratios are kept within [1 - clip_low, 1 + clip_high]
+ * (0 <= clip_low <= 1, 0 <= clip_high, both finite); kl (finite, >= 0) is the
+ * KL term's factor. */
+typedef struct {
+    const int32_t* action;
+    const float* old_logprob;
+    const float* ref_logprob;
+    const float* advantage;
+    float clip_low;
+    float clip_high;
+    float kl;
+    int32_t reserved;
+} gem_policy;
+
+/* Outputs of the policy loss, [rows] each; any may be NULL. */
+typedef struct {
+    float* loss;
+    float* logprob;       /* of the action */
+    float* ratio;
+    float* kl;            /* the KL term without its factor (0 without ref_logprob) */
+} gem_policy_terms;
+
+/* Clipped policy loss of each row: with lp the log probability of the action
+ * a under q = softmax(logits / temperature), A the advantage,
+ *     ratio = exp(lp - old_logprob),  d = ref_logprob - lp,  kl = e^d - 1 - d,
+ *     loss = -min(ratio A, clip(ratio) A) + p->kl kl.
+ * An advantage of 0 has no part in the loss, whatever the ratio.  weight
+ * ([rows], NULL: all 1) is the factor of the row's loss in what is minimised:
+ * it does not multiply loss[r], but a row of weight 0, or whose action is
+ * outside [0, vocab) (padding), has outputs of 0 and its logits are not read.
+ * An action whose logit is -inf has log probability -inf and ratio 0, and an
+ * infinite KL term.  A row with a NaN or +inf among its logits has NaN for
+ * them.  Errors: EINVAL, EDTYPE, EALIGN. */
+int gem_policy_loss(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, const float* weight,
+                    const gem_policy_terms* out);
+
+/* The same and its gradient: grad (rows x vocab of the logits' type,
+ * grad_stride elements between rows) receives
+ *     weight[r] / temperature * slope ([v = a] - q_v),
+ *     slope = -ratio A [where the minimum is the unclipped one's, equal ones
+ *             included] + p->kl (1 - e^d),
+ * zero in rows that do not count.  out may be NULL, or any of its arrays.  grad
+ * may be the logits' own memory (same address and stride).  A row whose slope
+ * is not finite has a gradient that is not.  Errors: EINVAL, EDTYPE, EALIGN. */
+int gem_policy_grad(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, const float* weight,
+                    const gem_policy_terms* out, void* grad, int64_t grad_stride);
 
 /* Inputs of the gated linear recurrence over `sequences` (>= 1) sequences of
  * tokens (0 to GEM_TOKENS_MAX) x channels, packed one after the other:

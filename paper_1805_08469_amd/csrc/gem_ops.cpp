@@ -1,5 +1,5 @@
 // gem_ops.cpp -- the C ABI of the worker's operators: handles and argument
-// checks.  Kernels live in gem_logits.hip and gem_scan.hip.
+// checks.  Kernels live in gem_logits.hip, gem_policy.hip and gem_scan.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -193,6 +193,46 @@ int gem_distill_grad(gem_ops_t* ops, const gem_logits* z, const gem_teacher* tea
 {
     if (!ops || !z || (!grad && z->rows > 0)) return GEM_EINVAL;
     return distill(ops, z, teacher, weight, loss, grad, grad_stride);
+}
+
+static int policy(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, const float* weight,
+                  const gem_policy_terms* out, void* grad, int64_t grad_stride)
+{
+    gemk::PolicyArgs a{};
+    const int rc = check_logits(z, &a.l);
+    if (rc != GEM_OK) return rc;
+    if (!p || !(p->clip_low >= 0.0f && p->clip_low <= 1.0f) || !(p->clip_high >= 0.0f) ||
+        !std::isfinite(p->clip_high) || !(p->kl >= 0.0f) || !std::isfinite(p->kl))
+        return GEM_EINVAL;
+    if (z->rows > 0 && (!p->action || !p->old_logprob || !p->advantage)) return GEM_EINVAL;
+    if (!row_stride(grad_stride, z->vocab, &a.grad_stride)) return GEM_EINVAL;
+    if (grad == z->data && grad && a.grad_stride != a.l.stride) return GEM_EINVAL;
+    if (out) a.out = *out;
+    if (!aligned(p->action, 4) || !aligned(p->old_logprob, 4) || !aligned(p->ref_logprob, 4) ||
+        !aligned(p->advantage, 4) || !aligned(weight, 4) || !aligned(a.out.loss, 4) ||
+        !aligned(a.out.logprob, 4) || !aligned(a.out.ratio, 4) || !aligned(a.out.kl, 4) ||
+        !aligned(grad, element(z->dtype)))
+        return GEM_EALIGN;
+    a.p = *p;
+    a.weight = weight;
+    a.grad = grad;
+    if (a.l.rows == 0) return GEM_OK;
+    OPS_HIP(gemk::launch_policy(a, z->dtype == GEM_BF16, ops->dev, ops->stream));
+    return GEM_OK;
+}
+
+int gem_policy_loss(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, const float* weight,
+                    const gem_policy_terms* out)
+{
+    if (!ops || !z || !out) return GEM_EINVAL;
+    return policy(ops, z, p, weight, out, nullptr, 0);
+}
+
+int gem_policy_grad(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, const float* weight,
+                    const gem_policy_terms* out, void* grad, int64_t grad_stride)
+{
+    if (!ops || !z || (!grad && z->rows > 0)) return GEM_EINVAL;
+    return policy(ops, z, p, weight, out, grad, grad_stride);
 }
 
 int gem_scan_scratch(int64_t tokens, int32_t channels, int64_t* bytes)

@@ -1,5 +1,5 @@
 // gem_ops.hpp -- pieces shared by the host side and the kernels of the worker's
-// operators (scores of logits, distillation, the gated recurrence).
+// operators.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -48,6 +48,15 @@ struct DistillArgs {
     int64_t grad_stride;
 };
 
+struct PolicyArgs {
+    LogitArgs l;
+    gem_policy p;
+    const float* weight;   // [rows] or null
+    gem_policy_terms out;
+    void* grad;            // rows x vocab, or null: the loss alone
+    int64_t grad_stride;
+};
+
 struct ScanArgs {
     gem_scan s;            // strides filled in
     void* y;
@@ -79,6 +88,7 @@ struct OpsDevice {
 
 hipError_t launch_scores(const ScoreArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_distill(const DistillArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
+hipError_t launch_policy(const PolicyArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 int64_t scan_rows(int64_t tokens, int64_t channels);
 int64_t scan_bytes(int64_t tokens, int64_t channels);            // of a launch
 int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);    // of it and of any smaller one

@@ -53,7 +53,7 @@ EXPORTED = (
     "gem_pi_hist_start", "gem_pi_hist_start_segments", "gem_pi_hist_read", "gem_set_segments",
     "gem_set_cache_policy", "gem_dims", "gem_gather_static",
     "gem_ops_create", "gem_ops_destroy", "gem_token_scores", "gem_distill_loss",
-    "gem_distill_grad", "gem_scan_scratch", "gem_scan_state_rows", "gem_scan_forward",
+    "gem_distill_grad", "gem_policy_loss", "gem_policy_grad", "gem_scan_scratch", "gem_scan_state_rows", "gem_scan_forward",
     "gem_scan_backward",
 )
 
@@ -97,6 +97,17 @@ class gem_scores(C.Structure):
 class gem_teacher(C.Structure):
     _fields_ = [("ids", C.c_void_p), ("logprob", C.c_void_p), ("k", C.c_int32),
                 ("tail", C.c_int32)]
+
+
+class gem_policy(C.Structure):
+    _fields_ = [("action", C.c_void_p), ("old_logprob", C.c_void_p), ("ref_logprob", C.c_void_p),
+                ("advantage", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("kl", C.c_float), ("reserved", C.c_int32)]
+
+
+class gem_policy_terms(C.Structure):
+    _fields_ = [("loss", C.c_void_p), ("logprob", C.c_void_p), ("ratio", C.c_void_p),
+                ("kl", C.c_void_p)]
 
 
 class gem_scan(C.Structure):
@@ -171,6 +182,10 @@ def _load():
         "gem_distill_loss": (C.c_int, [vp, C.POINTER(gem_logits), C.POINTER(gem_teacher), vp, vp]),
         "gem_distill_grad": (C.c_int, [vp, C.POINTER(gem_logits), C.POINTER(gem_teacher), vp, vp,
                                        vp, C.c_int64]),
+        "gem_policy_loss": (C.c_int, [vp, C.POINTER(gem_logits), C.POINTER(gem_policy), vp,
+                                      C.POINTER(gem_policy_terms)]),
+        "gem_policy_grad": (C.c_int, [vp, C.POINTER(gem_logits), C.POINTER(gem_policy), vp,
+                                      C.POINTER(gem_policy_terms), vp, C.c_int64]),
         "gem_scan_scratch": (C.c_int, [C.c_int64, C.c_int32, i64p]),
         "gem_scan_state_rows": (C.c_int, [C.c_int64, i64p]),
         "gem_scan_forward": (C.c_int, [vp, C.POINTER(gem_scan), vp, C.c_int64, vp, vp]),
@@ -455,6 +470,17 @@ def gem_distill_grad(ops: int, z: gem_logits, teacher: gem_teacher, weight: int,
            "gem_distill_grad")
 
 
+def gem_policy_loss(ops: int, z: gem_logits, p: gem_policy, weight: int, out: gem_policy_terms) -> None:
+    _check(_L.gem_policy_loss(ops, C.byref(z), C.byref(p), weight, C.byref(out)), "gem_policy_loss")
+
+
+def gem_policy_grad(ops: int, z: gem_logits, p: gem_policy, weight: int,
+                    out: gem_policy_terms | None, grad: int, grad_stride: int) -> None:
+    _check(_L.gem_policy_grad(ops, C.byref(z), C.byref(p), weight,
+                              C.byref(out) if out is not None else None, grad, grad_stride),
+           "gem_policy_grad")
+
+
 def gem_scan_scratch(tokens: int, channels: int) -> int:
     out = C.c_int64()
     _check(_L.gem_scan_scratch(tokens, channels, C.byref(out)), "gem_scan_scratch")
@@ -590,6 +616,22 @@ class Ops:
                      temperature=1.0, tail=0, weight=None, grad_stride=0):
         gem_distill_grad(self.h, gem_logits(data, rows, stride, vocab, dtype, temperature, 0),
                          gem_teacher(ids, teacher, k, tail), weight, loss, grad, grad_stride)
+
+    def policy_loss(self, data, rows, vocab, dtype, action, old_logprob, advantage,
+                    ref_logprob=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, stride=0,
+                    temperature=1.0, weight=None, loss=None, logprob=None, ratio=None, kl=None):
+        gem_policy_loss(self.h, gem_logits(data, rows, stride, vocab, dtype, temperature, 0),
+                        gem_policy(action, old_logprob, ref_logprob, advantage, clip_low, clip_high,
+                                   kl_coef, 0), weight, gem_policy_terms(loss, logprob, ratio, kl))
+
+    def policy_grad(self, data, rows, vocab, dtype, action, old_logprob, advantage, grad,
+                    ref_logprob=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, stride=0,
+                    temperature=1.0, weight=None, loss=None, logprob=None, ratio=None, kl=None,
+                    grad_stride=0):
+        gem_policy_grad(self.h, gem_logits(data, rows, stride, vocab, dtype, temperature, 0),
+                        gem_policy(action, old_logprob, ref_logprob, advantage, clip_low, clip_high,
+                                   kl_coef, 0), weight, gem_policy_terms(loss, logprob, ratio, kl),
+                        grad, grad_stride)
 
     def scan_forward(self, x, gate, tokens, channels, sequences, dtype, y, offsets=None, h0=None,
                      h_last=None, states=None, x_stride=0, gate_stride=0, y_stride=0):

@@ -406,8 +406,8 @@ int gem_copy_f32(const float* src, float* dst, int64_t count, void* stream);
  * What a worker computes from data before it has an update to commit: the
  * scores of a model's logits (a teacher's record, an evaluation), the
  * distillation loss against such a record and the clipped loss of a policy,
- * each with its gradient, and a gated linear recurrence with its backward
- * pass.  Unlike the commits, which are
+ * each with its gradient, an embedding and a gated linear recurrence with
+ * their backward passes.  Unlike the commits, which are
  * held to fixed bits, their values are those of the formulas up to rounding:
  * inputs are binary32 or bfloat16 (GEM_F32, GEM_BF16), sums, states and
  * statistics are binary32, and outputs of the inputs' type are rounded once
@@ -433,8 +433,8 @@ typedef struct gem_ops_handle gem_ops_t;
 
 /* Create the handle on the current device.  stream is the hipStream_t its work
  * is queued on (NULL: the device's null stream) and must outlive it.
- * scratch_bytes is the largest gem_scan_scratch of the recurrences it is used
- * for, 0 if none.  Errors: EINVAL, ENOMEM, EHIP. */
+ * scratch_bytes is the largest that gem_scan_scratch, gem_embed_scratch and
+ * their like ask for what it is used for, 0 if none.  Errors: EINVAL, ENOMEM, EHIP. */
 int gem_ops_create(int64_t scratch_bytes, void* stream, gem_ops_t** out);
 
 /* Free the scratch (after the stream drains) and the handle. */
@@ -567,6 +567,40 @@ int gem_policy_loss(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, co
  * is not finite has a gradient that is not.  Errors: EINVAL, EDTYPE, EALIGN. */
 int gem_policy_grad(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, const float* weight,
                     const gem_policy_terms* out, void* grad, int64_t grad_stride);
+
+/* An embedding: a table of vocab (1 to GEM_VOCAB_MAX) x dim, and count (0 to
+ * GEM_TOKENS_MAX) tokens.  dtype is the table's, or its gradient's; scale
+ * (finite) multiplies every row. */
+typedef struct {
+    const void* table;
+    const int32_t* tokens;
+    int64_t count;
+    int64_t stride;       /* of the table */
+    int32_t vocab;
+    int32_t dim;
+    int32_t dtype;
+    float scale;
+} gem_embed;
+
+/* out[t] = scale * table[tokens[t]] (count x dim of out_dtype); zeros for a
+ * token outside [0, vocab) (padding).  Errors: EINVAL, EDTYPE, EALIGN. */
+int gem_embed_forward(gem_ops_t* ops, const gem_embed* e, void* out, int64_t out_stride,
+                      int32_t out_dtype);
+
+/* Scratch bytes that a gem_ops_t needs for gem_embed_backward of up to these
+ * sizes (smaller ones never need more). */
+int gem_embed_scratch(int64_t count, int32_t vocab, int32_t dim, int64_t* bytes);
+
+/* The table's gradient (e->dtype; e's table and stride are not looked at) from
+ * that of the rows (dout, count x dim of dout_dtype):
+ *     grad[v] = scale * sum of dout[t] over the places t of token v,
+ * zeros for a token that does not occur.  With add 1 that is added to what grad
+ * holds (a table that is the output matrix too has a gradient already), and
+ * rows of tokens that do not occur are neither read nor written.  Every
+ * sum is formed in one order that only the tokens decide.
+ * Errors: EINVAL, EDTYPE, EALIGN, ESCRATCH. */
+int gem_embed_backward(gem_ops_t* ops, const gem_embed* e, const void* dout, int64_t dout_stride,
+                       int32_t dout_dtype, void* grad, int64_t grad_stride, int32_t add);
 
 /* Inputs of the gated linear recurrence over `sequences` (>= 1) sequences of
  * tokens (0 to GEM_TOKENS_MAX) x channels, packed one after the other:

@@ -1,5 +1,5 @@
 // gem_ops.cpp -- the C ABI of the worker's operators: handles and argument
-// checks.  Kernels live in gem_logits.hip, gem_policy.hip and gem_scan.hip.
+// checks.  Kernels live in gem_logits.hip, gem_policy.hip, gem_embed.hip and gem_scan.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -80,6 +80,22 @@ int check_scan(const gem_scan* s, gem_scan* out)
     if (!aligned(s->x, element(s->dtype)) || !aligned(s->gate, element(s->dtype)) ||
         !aligned(s->offsets, 8) || !aligned(s->h0, 4))
         return GEM_EALIGN;
+    return GEM_OK;
+}
+
+int check_embed(const gem_embed* e, int32_t rows_dtype, const void* rows, int64_t rows_stride, gemk::EmbedArgs* a)
+{
+    if (!e) return GEM_EINVAL;
+    if ((e->dtype != GEM_F32 && e->dtype != GEM_BF16) || (rows_dtype != GEM_F32 && rows_dtype != GEM_BF16))
+        return GEM_EDTYPE;
+    if (e->count < 0 || e->count > GEM_TOKENS_MAX || e->vocab < 1 || e->vocab > GEM_VOCAB_MAX || e->dim < 1)
+        return GEM_EINVAL;
+    if (!std::isfinite(e->scale)) return GEM_EINVAL;
+    if (e->count > 0 && (!e->tokens || !rows)) return GEM_EINVAL;
+    if (!row_stride(rows_stride, e->dim, &a->rows_stride)) return GEM_EINVAL;
+    if (!aligned(e->tokens, 4) || !aligned(rows, element(rows_dtype))) return GEM_EALIGN;
+    a->e = *e;
+    a->rows = const_cast<void*>(rows);
     return GEM_OK;
 }
 
@@ -233,6 +249,45 @@ int gem_policy_grad(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, co
 {
     if (!ops || !z || (!grad && z->rows > 0)) return GEM_EINVAL;
     return policy(ops, z, p, weight, out, grad, grad_stride);
+}
+
+int gem_embed_forward(gem_ops_t* ops, const gem_embed* e, void* out, int64_t out_stride, int32_t out_dtype)
+{
+    if (!ops) return GEM_EINVAL;
+    gemk::EmbedArgs a{};
+    const int rc = check_embed(e, out_dtype, out, out_stride, &a);
+    if (rc != GEM_OK) return rc;
+    if (e->count > 0 && !e->table) return GEM_EINVAL;
+    if (!row_stride(e->stride, e->dim, &a.e.stride)) return GEM_EINVAL;
+    if (!aligned(e->table, element(e->dtype))) return GEM_EALIGN;
+    if (e->count == 0) return GEM_OK;
+    OPS_HIP(gemk::launch_embed_forward(a, e->dtype == GEM_BF16, out_dtype == GEM_BF16, ops->stream));
+    return GEM_OK;
+}
+
+int gem_embed_scratch(int64_t count, int32_t vocab, int32_t dim, int64_t* bytes)
+{
+    if (!bytes || count < 0 || count > GEM_TOKENS_MAX || vocab < 1 || vocab > GEM_VOCAB_MAX || dim < 1)
+        return GEM_EINVAL;
+    *bytes = gemk::embed_scratch_bytes(count, vocab, dim);
+    return GEM_OK;
+}
+
+int gem_embed_backward(gem_ops_t* ops, const gem_embed* e, const void* dout, int64_t dout_stride,
+                       int32_t dout_dtype, void* grad, int64_t grad_stride, int32_t add)
+{
+    if (!ops) return GEM_EINVAL;
+    gemk::EmbedArgs a{};
+    const int rc = check_embed(e, dout_dtype, dout, dout_stride, &a);
+    if (rc != GEM_OK) return rc;
+    if (!grad || (add != 0 && add != 1)) return GEM_EINVAL;
+    if (!row_stride(grad_stride, e->dim, &a.grad_stride)) return GEM_EINVAL;
+    if (!aligned(grad, element(e->dtype))) return GEM_EALIGN;
+    a.grad = grad;
+    a.add = add != 0;
+    if (gemk::embed_scratch_bytes(e->count, e->vocab, e->dim) > ops->dev.scan_bytes) return GEM_ESCRATCH;
+    OPS_HIP(gemk::launch_embed_backward(a, e->dtype == GEM_BF16, dout_dtype == GEM_BF16, ops->dev, ops->stream));
+    return GEM_OK;
 }
 
 int gem_scan_scratch(int64_t tokens, int32_t channels, int64_t* bytes)

@@ -12,7 +12,7 @@ namespace gemk {
 // Keeps the detail of a failed HIP call for gem_last_error (gem_api.cpp).
 void note_hip_error(const char* file, const char* what, hipError_t e, int line);
 
-// Scratch that every handle has, ahead of what gem_scan_scratch asks for.
+// Scratch that every handle has, ahead of what it was created with.
 constexpr int64_t kFixedScratch = int64_t{8} << 20;
 
 // Tokens between two kept states of a recurrence.
@@ -57,6 +57,15 @@ struct PolicyArgs {
     int64_t grad_stride;
 };
 
+struct EmbedArgs {
+    gem_embed e;           // stride filled in
+    void* rows;            // count x dim: the output, or its gradient
+    int64_t rows_stride;
+    void* grad;            // vocab x dim
+    int64_t grad_stride;
+    bool add;
+};
+
 struct ScanArgs {
     gem_scan s;            // strides filled in
     void* y;
@@ -82,13 +91,16 @@ struct ScanBackArgs {
 struct OpsDevice {
     int32_t cus;             // compute units
     void* scratch;           // kFixedScratch bytes
-    void* scan;              // scan_bytes bytes
+    void* scan;              // scan_bytes bytes, of every operator that asks for scratch
     int64_t scan_bytes;
 };
 
 hipError_t launch_scores(const ScoreArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_distill(const DistillArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 hipError_t launch_policy(const PolicyArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
+int64_t embed_scratch_bytes(int64_t count, int64_t vocab, int64_t dim);
+hipError_t launch_embed_forward(const EmbedArgs& a, bool bf16, bool rows_bf16, hipStream_t stream);
+hipError_t launch_embed_backward(const EmbedArgs& a, bool bf16, bool rows_bf16, const OpsDevice& d, hipStream_t stream);
 int64_t scan_rows(int64_t tokens, int64_t channels);
 int64_t scan_bytes(int64_t tokens, int64_t channels);            // of a launch
 int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);    // of it and of any smaller one

@@ -53,8 +53,9 @@ EXPORTED = (
     "gem_pi_hist_start", "gem_pi_hist_start_segments", "gem_pi_hist_read", "gem_set_segments",
     "gem_set_cache_policy", "gem_dims", "gem_gather_static",
     "gem_ops_create", "gem_ops_destroy", "gem_token_scores", "gem_distill_loss",
-    "gem_distill_grad", "gem_policy_loss", "gem_policy_grad", "gem_scan_scratch", "gem_scan_state_rows", "gem_scan_forward",
-    "gem_scan_backward",
+    "gem_distill_grad", "gem_policy_loss", "gem_policy_grad", "gem_embed_forward",
+    "gem_embed_scratch", "gem_embed_backward", "gem_scan_scratch", "gem_scan_state_rows",
+    "gem_scan_forward", "gem_scan_backward",
 )
 
 
@@ -108,6 +109,12 @@ class gem_policy(C.Structure):
 class gem_policy_terms(C.Structure):
     _fields_ = [("loss", C.c_void_p), ("logprob", C.c_void_p), ("ratio", C.c_void_p),
                 ("kl", C.c_void_p)]
+
+
+class gem_embed(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("tokens", C.c_void_p), ("count", C.c_int64),
+                ("stride", C.c_int64), ("vocab", C.c_int32), ("dim", C.c_int32),
+                ("dtype", C.c_int32), ("scale", C.c_float)]
 
 
 class gem_scan(C.Structure):
@@ -186,6 +193,10 @@ def _load():
                                       C.POINTER(gem_policy_terms)]),
         "gem_policy_grad": (C.c_int, [vp, C.POINTER(gem_logits), C.POINTER(gem_policy), vp,
                                       C.POINTER(gem_policy_terms), vp, C.c_int64]),
+        "gem_embed_forward": (C.c_int, [vp, C.POINTER(gem_embed), vp, C.c_int64, C.c_int32]),
+        "gem_embed_scratch": (C.c_int, [C.c_int64, C.c_int32, C.c_int32, i64p]),
+        "gem_embed_backward": (C.c_int, [vp, C.POINTER(gem_embed), vp, C.c_int64, C.c_int32, vp,
+                                         C.c_int64, C.c_int32]),
         "gem_scan_scratch": (C.c_int, [C.c_int64, C.c_int32, i64p]),
         "gem_scan_state_rows": (C.c_int, [C.c_int64, i64p]),
         "gem_scan_forward": (C.c_int, [vp, C.POINTER(gem_scan), vp, C.c_int64, vp, vp]),
@@ -481,6 +492,22 @@ def gem_policy_grad(ops: int, z: gem_logits, p: gem_policy, weight: int,
            "gem_policy_grad")
 
 
+def gem_embed_forward(ops: int, e: gem_embed, out: int, out_stride: int, out_dtype: int) -> None:
+    _check(_L.gem_embed_forward(ops, C.byref(e), out, out_stride, out_dtype), "gem_embed_forward")
+
+
+def gem_embed_scratch(count: int, vocab: int, dim: int) -> int:
+    out = C.c_int64()
+    _check(_L.gem_embed_scratch(count, vocab, dim, C.byref(out)), "gem_embed_scratch")
+    return out.value
+
+
+def gem_embed_backward(ops: int, e: gem_embed, dout: int, dout_stride: int, dout_dtype: int,
+                       grad: int, grad_stride: int, add: int) -> None:
+    _check(_L.gem_embed_backward(ops, C.byref(e), dout, dout_stride, dout_dtype, grad, grad_stride,
+                                 add), "gem_embed_backward")
+
+
 def gem_scan_scratch(tokens: int, channels: int) -> int:
     out = C.c_int64()
     _check(_L.gem_scan_scratch(tokens, channels, C.byref(out)), "gem_scan_scratch")
@@ -632,6 +659,16 @@ class Ops:
                         gem_policy(action, old_logprob, ref_logprob, advantage, clip_low, clip_high,
                                    kl_coef, 0), weight, gem_policy_terms(loss, logprob, ratio, kl),
                         grad, grad_stride)
+
+    def embed_forward(self, table, tokens, count, vocab, dim, dtype, out, out_dtype, scale=1.0,
+                      stride=0, out_stride=0):
+        gem_embed_forward(self.h, gem_embed(table, tokens, count, stride, vocab, dim, dtype, scale),
+                          out, out_stride, out_dtype)
+
+    def embed_backward(self, tokens, count, vocab, dim, dtype, dout, dout_dtype, grad, scale=1.0,
+                       dout_stride=0, grad_stride=0, add=0):
+        gem_embed_backward(self.h, gem_embed(None, tokens, count, 0, vocab, dim, dtype, scale),
+                           dout, dout_stride, dout_dtype, grad, grad_stride, add)
 
     def scan_forward(self, x, gate, tokens, channels, sequences, dtype, y, offsets=None, h0=None,
                      h_last=None, states=None, x_stride=0, gate_stride=0, y_stride=0):

@@ -1,0 +1,250 @@
+"""An embedding's rows and gradient against their definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paper_1805_08469_amd import gem as G
+
+U = 2.0 ** -24
+HALF = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
+KIND = {torch.float32: G.GEM_F32, torch.bfloat16: G.GEM_BF16}
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def wide(rows, cols, pad, dtype, value=0.0):
+    return torch.full((rows, cols + pad), value, device="cuda", dtype=dtype)
+
+
+def tokens_of(kind, count, vocab, g):
+    if kind == "one":                     # the same token everywhere
+        t = torch.full((count,), vocab // 2, device="cuda")
+    elif kind == "words":                 # frequencies of 1/rank
+        t = (torch.rand(count, device="cuda", generator=g, dtype=torch.float64) * math.log(vocab + 1)).exp().long() - 1
+        t = (t.clamp(0, vocab - 1) * 7919 + 3) % vocab
+    elif kind == "none":                  # nothing but padding
+        t = torch.randint(1, 9, (count,), device="cuda", generator=g) * -3
+    else:
+        t = torch.randint(vocab, (count,), device="cuda", generator=g)
+    if kind == "words":
+        t[1::7] = -1
+        t[3::11] = vocab
+        t[4::13] = 2 ** 31 - 1
+    return t.to(torch.int32)
+
+
+def backward(ops, tok, vocab, dout, grad, scale=1.0, add=0):
+    ops.embed_backward(tok.data_ptr(), tok.numel(), vocab, dout.shape[1], KIND[grad.dtype], dout=dout.data_ptr(),
+                       dout_dtype=KIND[dout.dtype], grad=grad.data_ptr(), scale=scale, dout_stride=dout.stride(0),
+                       grad_stride=grad.stride(0), add=add)
+
+
+def ops_for(count, vocab, dim, stream=None):
+    return G.Ops(G.gem_embed_scratch(count, vocab, dim), stream or torch.cuda.current_stream().cuda_stream)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("table,out", [(F32, F32), (F32, BF16), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("count,vocab,dim", [(1, 1, 1), (1, 50, 8), (5, 70, 7), (300, 500, 64), (257, 1000, 1001), (33, 9, 4104)])
+def test_lookup(count, vocab, dim, table, out):
+    g = torch.Generator(device="cuda").manual_seed(count)
+    for pad in (0, 3):
+        w = wide(vocab, dim, pad, table, 9.0)
+        w[:, :dim] = torch.randn(vocab, dim, device="cuda", generator=g)
+        tok = tokens_of("words", count, vocab, g)
+        y = wide(count, dim, pad, out, 7.0)
+        with G.Ops(0, torch.cuda.current_stream().cuda_stream) as ops:
+            ops.embed_forward(w.data_ptr(), tok.data_ptr(), count, vocab, dim, KIND[table], out=y.data_ptr(),
+                              out_dtype=KIND[out], scale=1.7, stride=w.stride(0), out_stride=y.stride(0))
+        have = (tok >= 0) & (tok < vocab)
+        # binary32 products, rounded once: the same as torch's.
+        want = w[torch.where(have, tok, 0).long(), :dim].float() * 1.7
+        want = torch.where(have[:, None], want, 0.0).to(out)
+        assert torch.equal(y[:, :dim], want)
+        assert (y[:, dim:] == 7).all()
+
+
+def want_of(tok, vocab, dout, scale):
+    """The sums in 64 bits, and their bounds: a sum of m terms is off by at most m + 2 roundings of the
+    sum of their sizes (m - 1 additions, however they are grouped, and the scale).  Added on the CPU:
+    atomics of 64 bits on one row take minutes."""
+    tok, rows = tok.cpu(), dout.cpu().double()
+    have = (tok >= 0) & (tok < vocab)
+    at, rows = tok[have].long(), rows[have]
+    total = torch.zeros(vocab, dout.shape[1], dtype=torch.float64).index_add_(0, at, rows).cuda()
+    size = torch.zeros(vocab, dout.shape[1], dtype=torch.float64).index_add_(0, at, rows.abs()).cuda()
+    m = torch.bincount(at, minlength=vocab).cuda().double()
+    total, err = total * scale, size * abs(scale) * U * (m[:, None] + 3)
+    return total, err, m > 0
+
+
+def check(grad, total, err):
+    off = (grad.double() - total).abs() - err - total.abs() * HALF[grad.dtype]
+    assert (off <= 0).all(), off.max().item()
+
+
+SIZES = [(1, 1, 1), (3, 5, 9), (63, 100, 8), (64, 100, 40), (65, 2, 515), (1500, 97, 130), (2047, 5003, 1001),
+         (8192, 300, 33), (8193, 300, 33), (20001, 70000, 17), (40000, 511, 64), (70003, 300000, 9)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,master", [(F32, F32), (BF16, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("count,vocab,dim", SIZES)
+def test_gradient(count, vocab, dim, rows, master):
+    """Written, and added to what is there; ranked and sorted; one token everywhere, none, words."""
+    for kind, pad in (("words", 0), ("one", 3), ("none", 0), ("even", 5)):
+        g = torch.Generator(device="cuda").manual_seed(count + pad)
+        tok = tokens_of(kind, count, vocab, g)
+        dout = wide(count, dim, pad, rows)[:, :dim]
+        dout.copy_(torch.randn(count, dim, device="cuda", generator=g))
+        grad = wide(vocab, dim, pad, master, 7.0)
+        with ops_for(count, vocab, dim) as ops:
+            backward(ops, tok, vocab, dout, grad[:, :dim], 0.3)
+            total, err, there = want_of(tok, vocab, dout, 0.3)
+            check(grad[:, :dim], total, err)
+            assert (grad[:, :dim][~there] == 0).all() and (grad[:, dim:] == 7).all()
+            again = torch.empty_like(grad)
+            backward(ops, tok, vocab, dout, again[:, :dim], 0.3)
+            assert torch.equal(again[:, :dim], grad[:, :dim])
+            base = torch.randn(vocab, dim + pad, device="cuda", generator=g).to(master)
+            grad = base.clone()
+            backward(ops, tok, vocab, dout, grad[:, :dim], 0.3, add=1)
+            both = total + base[:, :dim].double()
+            check(grad[:, :dim], both, err + U * both.abs())
+            assert torch.equal(grad[:, :dim][~there], base[:, :dim][~there]) and torch.equal(grad[:, dim:], base[:, dim:])
+
+
+@pytest.mark.gpu
+def test_gradient_is_that_of_the_lookup():
+    """<lookup(W), D> = <W, gradient(D)> for every D, which is all that a linear operator's gradient is."""
+    count, vocab, dim = 700, 90, 24
+    g = torch.Generator(device="cuda").manual_seed(2)
+    W, D = torch.randn(vocab, dim, device="cuda", generator=g), torch.randn(count, dim, device="cuda", generator=g)
+    tok = tokens_of("words", count, vocab, g)
+    y, grad = torch.empty_like(D), torch.empty_like(W)
+    with ops_for(count, vocab, dim) as ops:
+        ops.embed_forward(W.data_ptr(), tok.data_ptr(), count, vocab, dim, 0, out=y.data_ptr(), out_dtype=0, scale=2.5)
+        backward(ops, tok, vocab, D, grad, 2.5)
+    a, b = (y.double() * D.double()).sum(), (W.double() * grad.double()).sum()
+    assert abs(a - b) <= U * 400 * (W.double().abs() * grad.double().abs()).sum() + 1e-9
+
+
+@pytest.mark.gpu
+def test_no_places():
+    grad = torch.full((20, 11), 3.0, device="cuda")
+    tok, dout = torch.empty(0, device="cuda", dtype=torch.int32), torch.empty(0, 11, device="cuda")
+    with G.Ops(0, torch.cuda.current_stream().cuda_stream) as ops:
+        backward(ops, tok, 20, dout, grad, add=1)
+        assert (grad == 3).all()
+        backward(ops, tok, 20, dout, grad)
+        assert (grad == 0).all()
+        ops.embed_forward(grad.data_ptr(), None, 0, 20, 11, 0, out=None, out_dtype=0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [500, 30000])
+def test_two_graphs_share_a_scratch(count):
+    """Captured calls of one handle, replayed in turn with eager calls between."""
+    vocab, dim = 3000, 72
+    s = torch.cuda.Stream()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    sets = []
+    for i in range(2):
+        tok = tokens_of("words", count - 7 * i, vocab, g)
+        dout = torch.randn(tok.numel(), dim, device="cuda", generator=g).to(BF16)
+        sets.append((tok, dout, torch.zeros(vocab, dim, device="cuda")))
+    torch.cuda.synchronize()
+    with ops_for(count, vocab, dim, s.cuda_stream) as ops:
+        want, graphs = [], []
+        for tok, dout, grad in sets:
+            backward(ops, tok, vocab, dout, grad)
+            s.synchronize()
+            want.append(grad.clone())
+        for tok, dout, grad in sets:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                backward(ops, tok, vocab, dout, grad)
+            graphs.append(graph)
+        for _ in range(3):
+            for (tok, dout, grad), graph, w in zip(sets, graphs, want):
+                grad.fill_(5)
+                torch.cuda.synchronize()
+                with torch.cuda.stream(s):
+                    graph.replay()
+                s.synchronize()
+                assert torch.equal(grad, w)
+        del graphs
+
+
+@pytest.mark.gpu
+def test_more_elements_than_32_bits_count():
+    vocab, dim, count = 1050000, 2056, 40
+    grad = torch.full((vocab, dim), 1.0, device="cuda", dtype=BF16)
+    tok = torch.full((count,), vocab - 1, device="cuda", dtype=torch.int32)
+    tok[7] = 0
+    dout = torch.ones(count, dim, device="cuda")
+    with ops_for(count, vocab, dim) as ops:
+        backward(ops, tok, vocab, dout, grad)
+        assert (grad[-1] == count - 1).all() and (grad[0] == 1).all()
+        assert int(grad.count_nonzero()) == 2 * dim
+        out = torch.empty(count, dim, device="cuda")
+        ops.embed_forward(grad.data_ptr(), tok.data_ptr(), count, vocab, dim, 1, out=out.data_ptr(), out_dtype=0, scale=0.5)
+        assert (out[7] == 0.5).all() and (out[8] == (count - 1) / 2).all()
+
+
+def test_scratch_never_falls_as_sizes_grow():
+    before = 0
+    for count in sorted({max(0, n + d) for n in (0, 1, 32, 1024, 8192, 2 ** 15, 2 ** 20, 2 ** 20 + 5000, 2 ** 21, 2 ** 24, G.GEM_TOKENS_MAX - 1)
+                         for d in (-1, 0, 1)}):
+        now = G.gem_embed_scratch(count, 1000, 64)
+        assert now >= before, count
+        assert G.gem_embed_scratch(count, 1001, 64) >= now and G.gem_embed_scratch(count, 1000, 65) >= now
+        before = now
+    sizes = [G.gem_embed_scratch(n, 7, 3) for n in range(0, 3_000_000, 997)]
+    assert sizes == sorted(sizes)
+
+
+def test_refusals():
+    """On the host, before any work is queued."""
+    L, C, n = G.lib(), G.C, G.C.c_int64()
+    fake = 1 << 20
+
+
+    def e(**k):
+        d = dict(table=64, tokens=64, count=2, stride=0, vocab=10, dim=8, dtype=0, scale=1.0)
+        d.update(k)
+        return G.gem_embed(*d.values())
+
+    def forward(out=64, stride=0, dtype=0, ops=fake, **k):
+        x = e(**k)
+        return L.gem_embed_forward(ops, C.byref(x), out, stride, dtype)
+
+    def back(dout=64, stride=0, dtype=0, grad=64, gs=0, add=0, ops=fake, **k):
+        x = e(**k)
+        return L.gem_embed_backward(ops, C.byref(x), dout, stride, dtype, grad, gs, add)
+
+    assert L.gem_embed_forward(fake, None, 64, 0, 0) == L.gem_embed_backward(fake, None, 64, 0, 0, 64, 0, 0) == G.GEM_EINVAL
+    for f in (forward, back):
+        assert f(ops=None) == f(tokens=None) == f(count=-1) == f(count=2 ** 31 - 1) == f(vocab=0) == G.GEM_EINVAL
+        assert f(vocab=G.GEM_VOCAB_MAX + 1) == f(dim=0) == f(scale=math.inf) == f(scale=math.nan) == f(stride=7) == G.GEM_EINVAL
+        assert f(dtype=2) == G.GEM_EDTYPE
+        assert f(tokens=66) == G.GEM_EALIGN
+    assert forward(table=None) == forward(out=None) == G.GEM_EINVAL and forward(table=66) == forward(out=66) == G.GEM_EALIGN
+    assert forward(count=0, table=None, tokens=None, out=None) == G.GEM_OK
+    assert back(dout=None) == back(grad=None) == back(gs=7) == back(add=2) == G.GEM_EINVAL
+    assert back(dout=66) == back(grad=66) == G.GEM_EALIGN
+    x = e(dtype=3)
+    assert L.gem_embed_backward(fake, C.byref(x), 64, 0, 0, 64, 0, 0) == G.GEM_EDTYPE
+    for bad in ((-1, 1, 1), (2 ** 31 - 1, 1, 1), (1, 0, 1), (1, G.GEM_VOCAB_MAX + 1, 1), (1, 1, 0)):
+        assert L.gem_embed_scratch(*bad, C.byref(n)) == G.GEM_EINVAL
+    assert L.gem_embed_scratch(1, 1, 1, None) == G.GEM_EINVAL
+
+
+@pytest.mark.gpu
+def test_scratch_too_small():
+    with G.Ops(0, torch.cuda.current_stream().cuda_stream) as ops:
+        tok = torch.zeros(4, device="cuda", dtype=torch.int32)
+        x = torch.zeros(10, 8, device="cuda")
+        with pytest.raises(G.GemError) as err:
+            backward(ops, tok, 10, x[:4], x)
+        assert err.value.code == G.GEM_ESCRATCH

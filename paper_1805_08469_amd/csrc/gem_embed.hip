@@ -15,62 +15,76 @@ namespace gemk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCols = 8;                   // columns of a lane
+constexpr int kCols = 4;                   // columns of a lane: 16 bytes of binary32, next to its neighbours'
 
-// ---- eight elements at any address of their own alignment ------------------------------------
+// ---- four elements at any address of their own alignment --------------------------------------
 
-template <class T> using Raw = uint32_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-
-__device__ __forceinline__ void load8(const float* p, float (&v)[kCols])
-{
-    const Raw<float> a = reinterpret_cast<const Raw<float>*>(p)[0], b = reinterpret_cast<const Raw<float>*>(p)[1];
+template <class T> struct Vec;
+template <> struct Vec<float> {
+    using Type = uint32_t __attribute__((ext_vector_type(4), aligned(4)));
+    static __device__ __forceinline__ void widen(const Type& r, float (&v)[kCols])
+    {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[i] = __uint_as_float(a[i]);
-        v[4 + i] = __uint_as_float(b[i]);
+        for (int i = 0; i < kCols; ++i) v[i] = __uint_as_float(r[i]);
     }
-}
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[kCols])
-{
-    const Raw<uint16_t> a = *reinterpret_cast<const Raw<uint16_t>*>(p);
-    unpack(u32x4{a[0], a[1], a[2], a[3]}, v);
-}
-__device__ __forceinline__ void store8(float* p, const float (&v)[kCols])
-{
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        reinterpret_cast<Raw<float>*>(p)[h] = Raw<float>{__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]),
-                                                         __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
-}
-__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[kCols])
-{
-    const u32x4 r = pack(v);
-    *reinterpret_cast<Raw<uint16_t>*>(p) = Raw<uint16_t>{r[0], r[1], r[2], r[3]};
-}
-// The first n of them.
-template <class T> __device__ __forceinline__ void fetch(const T* p, int n, float (&v)[kCols])
-{
-    if (n >= kCols) {
-        load8(p, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) v[i] = i < n ? load(p, i) : 0.0f;
+    static __device__ __forceinline__ Type narrow(const float (&v)[kCols])
+    {
+        return Type{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
     }
-}
-template <class T> __device__ __forceinline__ void put(T* p, int n, const float (&v)[kCols])
+};
+template <> struct Vec<uint16_t> {
+    using Type = uint32_t __attribute__((ext_vector_type(2), aligned(2)));
+    static __device__ __forceinline__ void widen(const Type& r, float (&v)[kCols])
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v[2 * i] = __uint_as_float(r[i] << 16);
+            v[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+        }
+    }
+    static __device__ __forceinline__ Type narrow(const float (&v)[kCols])
+    {
+        return Type{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+    }
+};
+
+// A lane's columns of a row of `dim`: [c, c + kCols), of which it stores those from `from` on.  Past
+// the row's end it has the last ones again, so that loads are whole and stand in no branch; FEW: the
+// row has fewer than kCols.
+struct Cols {
+    int c, from, dim;
+    Cols() = default;
+    __device__ Cols(int at, int dim_) : c(at), from(at), dim(dim_)
+    {
+        if (c + kCols > dim) c = dim > kCols ? dim - kCols : 0;
+    }
+    __device__ bool any() const { return from < dim; }
+};
+template <class T, bool FEW> __device__ __forceinline__ typename Vec<T>::Type fetch(const T* row, const Cols& o)
 {
-    if (n >= kCols) {
-        store8(p, v);
+    if constexpr (!FEW) return *reinterpret_cast<const typename Vec<T>::Type*>(row + o.c);
+    typename Vec<T>::Type r{};
+    T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) e[i] = row[i < o.dim ? i : o.dim - 1];
+    return r;
+}
+// Non-temporal: 32768 x 2048 rows looked up 48 us instead of 52, their gradient 182 instead of 187.
+template <class T> __device__ __forceinline__ void put(T* row, const Cols& o, const float (&v)[kCols])
+{
+    if (o.from + kCols <= o.dim) {
+        __builtin_nontemporal_store(Vec<T>::narrow(v), reinterpret_cast<typename Vec<T>::Type*>(row + o.c));
     } else {
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
-            if (i < n) store(p, i, v[i]);
+            if (o.c + i >= o.from && o.c + i < o.dim) store(row, o.c + i, v[i]);
     }
 }
 
 // ---- lanes over rows ------------------------------------------------------------------------
 
-// Rows are taken in pieces of `lanes` (a power of two, at most 64) x 8 columns, by as many lanes.
+// Rows, or groups of them, are taken in pieces of Q x `lanes` (a power of two, at most 64) x kCols
+// columns, by as many lanes.
 struct Pieces {
     int lanes, of_row;
     int64_t rows;
@@ -80,26 +94,39 @@ __device__ __forceinline__ int64_t first_piece(const Pieces& p)
     return (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / p.lanes;
 }
 __device__ __forceinline__ int64_t piece_step(const Pieces& p) { return static_cast<int64_t>(gridDim.x) * (kThreads / p.lanes); }
-__device__ __forceinline__ int piece_col(const Pieces& p, int piece) { return (piece * p.lanes + static_cast<int>(threadIdx.x) % p.lanes) * kCols; }
+// The lane's q-th columns in a piece of Q.
+template <int Q> __device__ __forceinline__ Cols piece_cols(const Pieces& p, int piece, int q, int dim)
+{
+    return Cols(((piece * Q + q) * p.lanes + static_cast<int>(threadIdx.x) % p.lanes) * kCols, dim);
+}
 
 // ---- forward -------------------------------------------------------------------------------
 
-template <class T, class TO>
+// ROWS places a piece, all in flight: many for the rate, one where there are few places.
+template <class T, class TO, int ROWS, bool FEW>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(const EmbedArgs a, const Pieces p)
 {
     const int64_t n = p.rows * p.of_row;
     for (int64_t i = first_piece(p); i < n; i += piece_step(p)) {
-        const int64_t t = i / p.of_row;
-        const int col = piece_col(p, static_cast<int>(i - t * p.of_row)), left = a.e.dim - col;
-        if (left <= 0) continue;
-        const int token = a.e.tokens[t];
-        float v[kCols] = {};
-        if (token >= 0 && token < a.e.vocab) {
-            fetch(static_cast<const T*>(a.e.table) + token * a.e.stride + col, left, v);
+        const int64_t group = i / p.of_row, t = group * ROWS;
+        const Cols o = piece_cols<1>(p, static_cast<int>(i - group * p.of_row), 0, a.e.dim);
+        if (!o.any()) continue;
+        int token[ROWS];
+        typename Vec<T>::Type raw[ROWS];
 #pragma unroll
-            for (int k = 0; k < kCols; ++k) v[k] *= a.e.scale;
+        for (int u = 0; u < ROWS; ++u) token[u] = a.e.tokens[t + u < a.e.count ? t + u : a.e.count - 1];
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)         // padding: row 0, which is not used
+            raw[u] = fetch<T, FEW>(static_cast<const T*>(a.e.table) + (token[u] >= 0 && token[u] < a.e.vocab ? token[u] : 0) * a.e.stride, o);
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            float v[kCols];
+            Vec<T>::widen(raw[u], v);
+            const bool there = token[u] >= 0 && token[u] < a.e.vocab;
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) v[k] = there ? v[k] * a.e.scale : 0.0f;
+            if (t + u < a.e.count) put(static_cast<TO*>(a.rows) + (t + u) * a.rows_stride, o, v);
         }
-        put(static_cast<TO*>(a.rows) + t * a.rows_stride + col, left, v);
     }
 }
 
@@ -166,7 +193,8 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(const int32_t* token
 // of the places; each pass counts every tile's digits (count_kernel), and scatters behind what the
 // counts say stands ahead (scatter_kernel).
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
-constexpr int kSortWaves = kThreads / 64;
+constexpr int kSortThreads = kDigits, kSortWaves = kSortThreads / 64;
+constexpr int kHeld = 4, kShare = 64 * kHeld;      // places of a lane and a wave at a time
 
 struct Pass {
     const int32_t* keys;       // null: of the tokens
@@ -181,89 +209,118 @@ struct Pass {
     __device__ int digit(int key) const { return key >> shift & ((1 << bits) - 1); }
 };
 
-__global__ __launch_bounds__(kThreads) void count_kernel(const Pass p, Segment* seg)
+__global__ __launch_bounds__(kSortThreads) void count_kernel(const Pass p, Segment* seg)
 {
     __shared__ uint32_t counts[kDigits];
+    const int tid = threadIdx.x;
+    if (static_cast<int>(blockIdx.x) < p.tiles) {
+        counts[tid] = 0;
+        __syncthreads();
+        const int64_t from = static_cast<int64_t>(blockIdx.x) * p.tile;
+        const int64_t to = from + p.tile < p.n ? from + p.tile : p.n;
+        for (int64_t base = from; base < to; base += kHeld * kSortThreads) {
+            int key[kHeld];
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                const int64_t i = base + u * kSortThreads + tid;
+                key[u] = p.key(static_cast<int>(i < to ? i : to - 1));
+            }
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u)
+                if (base + u * kSortThreads + tid < to) atomicAdd(&counts[p.digit(key[u])], 1u);
+        }
+        __syncthreads();
+        p.counts[static_cast<int64_t>(blockIdx.x) * kDigits + tid] = counts[tid];
+    }
     clear(seg, p.vocab);
-    for (int d = threadIdx.x; d < kDigits; d += kThreads) counts[d] = 0;
-    __syncthreads();
-    if (static_cast<int>(blockIdx.x) >= p.tiles) return;
-    const int64_t from = static_cast<int64_t>(blockIdx.x) * p.tile;
-    const int to = from + p.tile < p.n ? static_cast<int>(from + p.tile) : p.n;
-    for (int64_t i = from + threadIdx.x; i < to; i += kThreads) atomicAdd(&counts[p.digit(p.key(static_cast<int>(i)))], 1u);
-    __syncthreads();
-    for (int d = threadIdx.x; d < kDigits; d += kThreads) p.counts[blockIdx.x * kDigits + d] = counts[d];
 }
 
-__global__ __launch_bounds__(kThreads) void scatter_kernel(const Pass p)
+__global__ __launch_bounds__(kSortThreads) void scatter_kernel(const Pass p)
 {
     __shared__ uint32_t next[kSortWaves][kDigits];     // where each wave's next place of a digit goes
-    __shared__ uint32_t totals[kThreads];
+    __shared__ uint32_t waves[kSortWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
     const int share = p.tile / kSortWaves;
     const int64_t from = static_cast<int64_t>(blockIdx.x) * p.tile + static_cast<int64_t>(wave) * share;
-    const int to = from + share < p.n ? static_cast<int>(from + share) : p.n;
-    for (int i = tid; i < kSortWaves * kDigits; i += kThreads) next[i / kDigits][i % kDigits] = 0;
-    __syncthreads();
-    for (int64_t i = from + lane; i < to; i += 64) atomicAdd(&next[wave][p.digit(p.key(static_cast<int>(i)))], 1u);
-    // Of a thread's two digits: the places in earlier tiles, and in all.
-    uint32_t before[2] = {}, all[2] = {};
-    const uint2* rows = reinterpret_cast<const uint2*>(p.counts) + tid;
-    const int mine = blockIdx.x;
-#pragma unroll 8
-    for (int t = 0; t < p.tiles; ++t) {
-        const uint2 c = rows[static_cast<int64_t>(t) * (kDigits / 2)];
-        before[0] += t < mine ? c.x : 0u;
-        before[1] += t < mine ? c.y : 0u;
-        all[0] += c.x;
-        all[1] += c.y;
-    }
-    totals[tid] = all[0] + all[1];
-    __syncthreads();
-    for (int s = 1; s < kThreads; s *= 2) {
-        const uint32_t add = tid >= s ? totals[tid - s] : 0u;
-        __syncthreads();
-        totals[tid] += add;
-        __syncthreads();
-    }
-    uint32_t at = totals[tid] - all[0] - all[1];
+    const int64_t to = from + share < p.n ? from + share : p.n;
+    int key[kHeld], place[kHeld];
+    const auto hold = [&](int64_t base) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        uint32_t base = at + before[k];
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = next[w][2 * tid + k];
-            next[w][2 * tid + k] = base;
-            base += c;
+        for (int u = 0; u < kHeld; ++u) {
+            const int64_t i = base + u * 64 + lane;
+            const int at = static_cast<int>(i < to ? i : to - 1);
+            key[u] = p.key(at);
+            place[u] = p.places ? p.places[at] : at;
         }
-        at += all[k];
+    };
+    if (from < to) hold(from);
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) next[w][tid] = 0;
+    // Of the thread's digit: the places in earlier tiles, and in all.
+    uint32_t before = 0, all = 0;
+    const int mine = blockIdx.x;
+#pragma unroll 16
+    for (int t = 0; t < p.tiles; ++t) {
+        const uint32_t c = p.counts[static_cast<int64_t>(t) * kDigits + tid];
+        before += t < mine ? c : 0u;
+        all += c;
+    }
+    uint32_t sum = all;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const uint32_t add = __shfl_up(sum, s);
+        sum += lane >= s ? add : 0u;
+    }
+    if (lane == 63) waves[wave] = sum;
+    __syncthreads();
+    for (int64_t base = from; base < to; base += kShare) {
+        if (base > from) hold(base);
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+            if (base + u * 64 + lane < to) atomicAdd(&next[wave][p.digit(key[u])], 1u);
+    }
+    if (share > kShare && from < to) hold(from);
+    __syncthreads();
+    uint32_t at = sum - all + before;
+    for (int w = 0; w < wave; ++w) at += waves[w];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t c = next[w][tid];
+        next[w][tid] = at;
+        at += c;
     }
     __syncthreads();
-    for (int64_t base = from; base < to; base += 64) {
-        const int64_t i = base + lane;
-        const bool in = i < to;
-        const int key = in ? p.key(static_cast<int>(i)) : 0, digit = p.digit(key);
-        uint64_t same = __ballot(in);
-        for (int b = 0; b < p.bits; ++b) {
-            const uint64_t set = __ballot(in && (digit >> b & 1));
-            same &= digit >> b & 1 ? set : ~set;
+    for (int64_t base = from; base < to; base += kShare) {
+        if (base > from) hold(base);
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            const bool in = base + u * 64 + lane < to;
+            const int digit = p.digit(key[u]);
+            uint64_t same = __ballot(in);          // of the lane's digit
+            for (int b = 0; b < p.bits; ++b) {
+                const uint64_t set = __ballot(in && (digit >> b & 1));
+                same &= digit >> b & 1 ? set : ~set;
+            }
+            const int first = __builtin_ctzll(same);
+            uint32_t start = 0;
+            if (in && lane == first) start = atomicAdd(&next[wave][digit], static_cast<uint32_t>(__builtin_popcountll(same)));
+            start = __shfl(start, first);
+            const uint32_t dest = start + __builtin_popcountll(same & ((uint64_t{1} << lane) - 1));
+            if (in) {
+                p.to_keys[dest] = key[u];
+                p.to_places[dest] = place[u];
+            }
         }
-        if (!in) continue;
-        const int first = __builtin_ctzll(same);
-        uint32_t start = 0;
-        if (lane == first) start = atomicAdd(&next[wave][digit], static_cast<uint32_t>(__builtin_popcountll(same)));
-        start = __shfl(start, first);
-        const uint32_t dest = start + __builtin_popcountll(same & ((uint64_t{1} << lane) - 1));
-        p.to_keys[dest] = key;
-        p.to_places[dest] = p.places ? p.places[i] : static_cast<int>(i);
     }
 }
 
 // ---- sums ------------------------------------------------------------------------------------
 
 // Chunks of kChunk sorted places that all have one token are summed ahead, and kChunk of such
-// chunks again, so that a row adds at most 2 kChunk places, as many chunks, and chunks of chunks.
+// chunks again, so that a row adds fewer than 2 kChunk places, as many chunks, and chunks of chunks.
 constexpr int kChunk = 32;
-constexpr int kTake = 8;                   // rows in flight
+constexpr int kTake = 16, kFew = 4;        // rows in flight
+constexpr int kGroup = 4;                  // rows of the table that lanes take together
 
 struct Sums {
     const int32_t* keys;
@@ -274,43 +331,39 @@ struct Sums {
     int n;
 };
 
-// v += rows [from, to) of f's, in their order.
-template <class F> __device__ __forceinline__ void add_rows(float (&v)[kCols], int from, int to, F f)
+// v += rows [from, to) of T, in their order, TAKE in flight; row(i) is where one begins.
+template <class T, bool FEW, int Q, int TAKE, class F>
+__device__ __forceinline__ void add_batches(float (&v)[Q][kCols], int& i, int to, const Cols (&o)[Q], F row)
 {
-    int i = from;
-    for (; i + kTake <= to; i += kTake) {
-        float x[kTake][kCols];
+    for (; i + (TAKE == kFew ? 1 : TAKE) <= to; i += TAKE) {
+        const T* at[TAKE];
+        typename Vec<T>::Type raw[TAKE][Q];
 #pragma unroll
-        for (int u = 0; u < kTake; ++u) f(i + u, x[u]);
+        for (int u = 0; u < TAKE; ++u) at[u] = row(TAKE > kFew || i + u < to ? i + u : to - 1);
 #pragma unroll
-        for (int u = 0; u < kTake; ++u)
+        for (int u = 0; u < TAKE; ++u)
 #pragma unroll
-            for (int k = 0; k < kCols; ++k) v[k] += x[u][k];
-    }
-    for (; i < to; ++i) {
-        float x[kCols];
-        f(i, x);
+            for (int q = 0; q < Q; ++q) raw[u][q] = fetch<T, FEW>(at[u], o[q]);
 #pragma unroll
-        for (int k = 0; k < kCols; ++k) v[k] += x[k];
+        for (int u = 0; u < TAKE; ++u)
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                float x[kCols];
+                Vec<T>::widen(raw[u][q], x);
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) v[q][k] += TAKE > kFew || i + u < to ? x[k] : 0.0f;
+            }
     }
 }
+// The last few with the very last again where there are fewer than kFew.
+template <class T, bool FEW, int Q, class F>
+__device__ __forceinline__ void add_rows(float (&v)[Q][kCols], int from, int to, const Cols (&o)[Q], F row)
+{
+    if constexpr (Q == 1) add_batches<T, FEW, Q, kTake>(v, from, to, o, row);
+    add_batches<T, FEW, Q, kFew>(v, from, to, o, row);
+}
 
-template <class T> struct Places {
-    const T* rows;
-    int64_t stride;
-    const int32_t* places;
-    int col, left;
-
-    __device__ void operator()(int i, float (&x)[kCols]) const { fetch(rows + places[i] * stride + col, left, x); }
-};
-struct Chunks {
-    const float* rows;
-    int dim, col, left;
-
-    __device__ void operator()(int i, float (&x)[kCols]) const { fetch(rows + static_cast<int64_t>(i) * dim + col, left, x); }
-};
-
-template <class T>
+template <class T, bool FEW>
 __global__ __launch_bounds__(kThreads) void chunk_kernel(const EmbedArgs a, const Pieces p, const Sums s)
 {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < s.n; i += static_cast<int64_t>(gridDim.x) * kThreads) {
@@ -322,82 +375,137 @@ __global__ __launch_bounds__(kThreads) void chunk_kernel(const EmbedArgs a, cons
     const int64_t n = p.rows * p.of_row;
     for (int64_t i = first_piece(p); i < n; i += piece_step(p)) {
         const int c = static_cast<int>(i / p.of_row);
-        const int col = piece_col(p, static_cast<int>(i - static_cast<int64_t>(c) * p.of_row)), left = a.e.dim - col;
-        const int from = c * kChunk, key = s.keys[from];
-        if (left <= 0 || key >= a.e.vocab || s.keys[from + kChunk - 1] != key) continue;
-        float v[kCols] = {};
-        add_rows(v, from, from + kChunk, Places<T>{static_cast<const T*>(a.rows), a.rows_stride, s.places, col, left});
-        put(s.chunks + static_cast<int64_t>(c) * a.e.dim + col, left, v);
+        const Cols o[1] = {piece_cols<1>(p, static_cast<int>(i - static_cast<int64_t>(c) * p.of_row), 0, a.e.dim)};
+        const int from = c * kChunk, key = s.keys[from], last = s.keys[from + kChunk - 1];
+        if (!o[0].any() || key >= a.e.vocab || last != key) continue;
+        float v[1][kCols] = {};
+        add_rows<T, FEW>(v, from, from + kChunk, o,
+                         [&](int j) { return static_cast<const T*>(a.rows) + s.places[j] * a.rows_stride; });
+        put(s.chunks + static_cast<int64_t>(c) * a.e.dim, o[0], v[0]);
     }
 }
 
+template <bool FEW>
 __global__ __launch_bounds__(kThreads) void big_chunk_kernel(const EmbedArgs a, const Pieces p, const Sums s)
 {
     const int64_t n = p.rows * p.of_row;
     for (int64_t i = first_piece(p); i < n; i += piece_step(p)) {
         const int c = static_cast<int>(i / p.of_row);
-        const int col = piece_col(p, static_cast<int>(i - static_cast<int64_t>(c) * p.of_row)), left = a.e.dim - col;
-        const int from = c * kChunk * kChunk, key = s.keys[from];
-        if (left <= 0 || key >= a.e.vocab || s.keys[from + kChunk * kChunk - 1] != key) continue;
-        float v[kCols] = {};
-        add_rows(v, c * kChunk, (c + 1) * kChunk, Chunks{s.chunks, a.e.dim, col, left});
-        put(s.big + static_cast<int64_t>(c) * a.e.dim + col, left, v);
+        const Cols o[1] = {piece_cols<1>(p, static_cast<int>(i - static_cast<int64_t>(c) * p.of_row), 0, a.e.dim)};
+        const int from = c * kChunk * kChunk, key = s.keys[from], last = s.keys[from + kChunk * kChunk - 1];
+        if (!o[0].any() || key >= a.e.vocab || last != key) continue;
+        float v[1][kCols] = {};
+        add_rows<float, FEW>(v, c * kChunk, (c + 1) * kChunk, o,
+                             [&](int j) { return s.chunks + static_cast<int64_t>(j) * a.e.dim; });
+        put(s.big + static_cast<int64_t>(c) * a.e.dim, o[0], v[0]);
     }
 }
 
-// v += the sorted places [lo, hi), in their order, from whole chunks where there are any.
-template <class T>
-__device__ __forceinline__ void add_segment(float (&v)[kCols], const EmbedArgs& a, const Sums& s, int lo, int hi, int col, int left)
+// A token's whole chunks [c0, c1); none if c0 >= c1.
+struct Whole {
+    int c0, c1;
+    __device__ explicit Whole(const Segment& g) : c0((g.lo + kChunk - 1) / kChunk), c1(g.hi / kChunk) {}
+    __device__ bool any() const { return c0 < c1; }
+};
+
+// v += the sorted places of a token with whole chunks, in their order.
+template <class T, bool FEW>
+__device__ __forceinline__ void add_long(float (&v)[1][kCols], const EmbedArgs& a, const Sums& s, const Segment& g, const Cols (&o)[1])
 {
-    const Places<T> places{static_cast<const T*>(a.rows), a.rows_stride, s.places, col, left};
-    const int c0 = (lo + kChunk - 1) / kChunk, c1 = hi / kChunk;
-    if (c0 >= c1) {
-        add_rows(v, lo, hi, places);
+    const auto place = [&](int j) { return static_cast<const T*>(a.rows) + s.places[j] * a.rows_stride; };
+    const auto chunk = [&](int j) { return s.chunks + static_cast<int64_t>(j) * a.e.dim; };
+    const Whole w(g);
+    const int b0 = (w.c0 + kChunk - 1) / kChunk, b1 = w.c1 / kChunk;
+    const bool big = s.big && b0 < b1;
+    add_rows<T, FEW>(v, g.lo, w.c0 * kChunk, o, place);
+    add_rows<float, FEW>(v, w.c0, big ? b0 * kChunk : w.c1, o, chunk);
+    if (big) {
+        add_rows<float, FEW>(v, b0, b1, o, [&](int j) { return s.big + static_cast<int64_t>(j) * a.e.dim; });
+        add_rows<float, FEW>(v, b1 * kChunk, w.c1, o, chunk);
+    }
+    add_rows<T, FEW>(v, w.c1 * kChunk, g.hi, o, place);
+}
+
+template <class TG, bool FEW, bool ADD, int Q>
+__device__ __forceinline__ void write(TG* to, const Cols (&o)[Q], float (&v)[Q][kCols], float scale)
+{
+    float x[Q][kCols] = {};
+    if constexpr (ADD) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) Vec<TG>::widen(fetch<TG, FEW>(to, o[q]), x[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) v[q][k] = v[q][k] * scale + x[q][k];
+        put(to, o[q], v[q]);
+    }
+}
+
+// The first `ahead` blocks: rows of tokens with whole chunks, each by the lanes that find the first
+// of them.  The others: all rows, or (ADD: added to what is there) those of tokens that occur, each
+// of which goes to the first of its sorted places.  kGroup rows are taken by the same lanes, and
+// the zeros of tokens that do not occur, which are most, are on their way before the first sum.
+// They lie far apart, since frequent tokens are often neighbours.
+template <class T, class TG, bool FEW, bool ADD, int Q>
+__global__ __launch_bounds__(kThreads) void rows_kernel(const EmbedArgs a, const Pieces p, const Pieces ahead, int blocks_ahead, const Sums s)
+{
+    if (static_cast<int>(blockIdx.x) < blocks_ahead) {
+        const int64_t n = ahead.rows * ahead.of_row, step = static_cast<int64_t>(blocks_ahead) * (kThreads / ahead.lanes);
+        for (int64_t i = first_piece(ahead); i < n; i += step) {
+            const int c = static_cast<int>(i / ahead.of_row);
+            const Cols o[1] = {piece_cols<1>(ahead, static_cast<int>(i - static_cast<int64_t>(c) * ahead.of_row), 0, a.e.dim)};
+            const int from = c * kChunk, key = s.keys[from], last = s.keys[from + kChunk - 1];
+            if (!o[0].any() || key >= a.e.vocab || last != key) continue;
+            const Segment g = s.seg[key];
+            if (Whole(g).c0 != c) continue;
+            float v[1][kCols] = {};
+            add_long<T, FEW>(v, a, s, g, o);
+            write<TG, FEW, ADD>(static_cast<TG*>(a.grad) + key * a.grad_stride, o, v, a.e.scale);
+        }
         return;
     }
-    add_rows(v, lo, c0 * kChunk, places);
-    const Chunks chunks{s.chunks, a.e.dim, col, left};
-    const int b0 = (c0 + kChunk - 1) / kChunk, b1 = c1 / kChunk;
-    if (!s.big || b0 >= b1) {
-        add_rows(v, c0, c1, chunks);
-    } else {
-        add_rows(v, c0, b0 * kChunk, chunks);
-        add_rows(v, b0, b1, Chunks{s.big, a.e.dim, col, left});
-        add_rows(v, b1 * kChunk, c1, chunks);
-    }
-    add_rows(v, c1 * kChunk, hi, places);
-}
-
-// Every row of the table's gradient, or (ADD) those of tokens that occur, added to what is there:
-// a row then goes to the first of its sorted places.
-template <class T, class TG, bool ADD>
-__global__ __launch_bounds__(kThreads) void rows_kernel(const EmbedArgs a, const Pieces p, const Sums s)
-{
-    const int64_t n = p.rows * p.of_row;
-    for (int64_t i = first_piece(p); i < n; i += piece_step(p)) {
-        const int row = static_cast<int>(i / p.of_row);
-        const int col = piece_col(p, static_cast<int>(i - static_cast<int64_t>(row) * p.of_row)), left = a.e.dim - col;
-        if (left <= 0) continue;
-        int token = row;
-        if (ADD) {
-            token = s.keys[row];
-            if (token >= a.e.vocab || (row > 0 && s.keys[row - 1] == token)) continue;
-        }
-        TG* to = static_cast<TG*>(a.grad) + token * a.grad_stride + col;
-        const Segment g = s.n ? s.seg[token] : Segment{0, 0};
-        float v[kCols] = {};
-        if (g.hi > g.lo) {
-            add_segment<T>(v, a, s, g.lo, g.hi, col, left);
+    const int64_t n = p.rows * p.of_row, behind = static_cast<int64_t>(blocks_ahead) * (kThreads / p.lanes);
+    for (int64_t i = first_piece(p) - behind; i < n; i += piece_step(p) - behind) {
+        const int64_t group = i / p.of_row;
+        Cols o[Q];
 #pragma unroll
-            for (int k = 0; k < kCols; ++k) v[k] *= a.e.scale;
+        for (int q = 0; q < Q; ++q) o[q] = piece_cols<Q>(p, static_cast<int>(i - group * p.of_row), q, a.e.dim);
+        const int64_t rows = ADD ? s.n : a.e.vocab;
+        const auto row_at = [&](int u) { return group + u * p.rows; };
+        const auto segment = [&](int u, int& token) {
+            Segment g{0, 0};
+            if (row_at(u) >= rows || !s.n) return g;
+            token = static_cast<int>(row_at(u));
             if (ADD) {
-                float x[kCols];
-                fetch(to, left, x);
-#pragma unroll
-                for (int k = 0; k < kCols; ++k) v[k] += x[k];
+                const int at = token;
+                token = s.keys[at];
+                if (token >= a.e.vocab || (at > 0 && s.keys[at - 1] == token)) return g;
             }
+            return s.seg[token];
+        };
+        if constexpr (!ADD) {
+            Segment g[kGroup];
+            int token;
+#pragma unroll
+            for (int u = 0; u < kGroup; ++u) g[u] = segment(u, token);
+            const float none[kCols] = {};
+#pragma unroll
+            for (int u = 0; u < kGroup; ++u)
+                if (row_at(u) < rows && g[u].hi == g[u].lo) {
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) put(static_cast<TG*>(a.grad) + row_at(u) * a.grad_stride, o[q], none);
+                }
         }
-        put(to, left, v);
+#pragma unroll 1
+        for (int u = 0; u < kGroup; ++u) {
+            int token;
+            const Segment g = segment(u, token);
+            if (g.hi == g.lo || Whole(g).any()) continue;
+            float v[Q][kCols] = {};
+            add_rows<T, FEW>(v, g.lo, g.hi, o, [&](int j) { return static_cast<const T*>(a.rows) + s.places[j] * a.rows_stride; });
+            write<TG, FEW, ADD>(static_cast<TG*>(a.grad) + token * a.grad_stride, o, v, a.e.scale);
+        }
     }
 }
 
@@ -405,12 +513,12 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const EmbedArgs a, const
 
 int64_t over(int64_t n, int64_t part) { return (n + part - 1) / part; }
 
-Pieces pieces_of(int64_t rows, int dim)
+Pieces pieces_of(int64_t rows, int dim, int quads = 1)
 {
     Pieces p;
     p.lanes = 1;
     while (p.lanes < 64 && p.lanes * kCols < dim) p.lanes *= 2;
-    p.of_row = static_cast<int>(over(dim, p.lanes * kCols));
+    p.of_row = static_cast<int>(over(dim, quads * p.lanes * kCols));
     p.rows = rows;
     return p;
 }
@@ -429,14 +537,10 @@ int bits_of(int vocab)         // of keys up to vocab
     return b;
 }
 
-// Places of a block in a pass of the sort: each wave has at least kShare, and there are no more
-// tiles than kTilesMost, since every block reads all tiles' counts.
-constexpr int64_t kShare = 512, kTilesMost = 512;
-int64_t tile_of(int64_t n)
-{
-    const int64_t least = kSortWaves * kShare, part = over(over(n, kTilesMost), kThreads) * kThreads;
-    return part > least ? part : least;
-}
+// Places of a block in a pass of the sort: no more tiles than kTilesMost, since every block reads
+// all tiles' counts.
+constexpr int64_t kTileLeast = kSortWaves * kShare, kTilesMost = 512;
+int64_t tile_of(int64_t n) { return over(over(n, kTilesMost) + (n == 0), kTileLeast) * kTileLeast; }
 
 // The parts of the scratch, in this order: two sorts' keys and places, counts, segments, chunks.
 struct Layout {
@@ -447,7 +551,7 @@ struct Layout {
         const auto up = [](int64_t b) { return over(b, 256) * 256; };
         order = up(n * 4);
         counts = 4 * order;
-        const int64_t tiles = over(n, kSortWaves * kShare);
+        const int64_t tiles = over(n, kTileLeast);
         seg = counts + up((tiles < kTilesMost ? tiles : kTilesMost) * kDigits * 4);
         chunks = seg + up(vocab * static_cast<int64_t>(sizeof(Segment)));
         big = chunks + up(n / kChunk * dim * 4);
@@ -459,11 +563,15 @@ struct Layout {
 // From this many places on chunks of chunks are worth a launch.
 constexpr int kBigLeast = 1 << 14;
 
-template <class T> hipError_t forward(const EmbedArgs& a, bool out_bf16, hipStream_t stream)
+template <class T, class TO, bool FEW> hipError_t forward(const EmbedArgs& a, hipStream_t stream)
 {
-    const Pieces p = pieces_of(a.e.count, a.e.dim);
-    if (out_bf16) hipLaunchKernelGGL((lookup_kernel<T, uint16_t>), grid_of(p), dim3(kThreads), 0, stream, a, p);
-    else hipLaunchKernelGGL((lookup_kernel<T, float>), grid_of(p), dim3(kThreads), 0, stream, a, p);
+    constexpr int ROWS = 4;
+    const Pieces each = pieces_of(a.e.count, a.e.dim), p = pieces_of(over(a.e.count, ROWS), a.e.dim);
+    // Enough pieces of several rows for four waves a SIMD.
+    if (p.rows * p.of_row * p.lanes >= int64_t{64} * 4096)
+        hipLaunchKernelGGL((lookup_kernel<T, TO, ROWS, FEW>), grid_of(p), dim3(kThreads), 0, stream, a, p);
+    else
+        hipLaunchKernelGGL((lookup_kernel<T, TO, 1, FEW>), grid_of(each), dim3(kThreads), 0, stream, a, each);
     return hipGetLastError();
 }
 
@@ -492,15 +600,26 @@ void sort(const EmbedArgs& a, const Layout& l, char* scratch, Sums& s, hipStream
         p.bits = static_cast<int>(over(bits - p.shift, passes - i));
         p.to_keys = order[2 * at];
         p.to_places = order[2 * at + 1];
-        hipLaunchKernelGGL(count_kernel, dim3(static_cast<unsigned>(p.tiles)), dim3(kThreads), 0, stream, p, i == 0 ? seg : nullptr);
-        hipLaunchKernelGGL(scatter_kernel, dim3(static_cast<unsigned>(p.tiles)), dim3(kThreads), 0, stream, p);
+        const int64_t clears = i == 0 && seg ? over(a.e.vocab, kSortThreads) : 0;
+        hipLaunchKernelGGL(count_kernel, dim3(static_cast<unsigned>(clears > p.tiles ? clears : p.tiles)), dim3(kSortThreads), 0,
+                           stream, p, i == 0 ? seg : nullptr);
+        hipLaunchKernelGGL(scatter_kernel, dim3(static_cast<unsigned>(p.tiles)), dim3(kSortThreads), 0, stream, p);
         p.shift += p.bits;
         p.keys = s.keys = p.to_keys;
         p.places = s.places = p.to_places;
     }
 }
 
-template <class T, class TG> hipError_t backward(const EmbedArgs& a, const OpsDevice& d, hipStream_t stream)
+template <class T, class TG, bool FEW, bool ADD, int Q>
+void rows(const EmbedArgs& a, const Sums& s, hipStream_t stream)
+{
+    const Pieces p = pieces_of(over(ADD ? s.n : a.e.vocab, kGroup), a.e.dim, Q), ahead = pieces_of(s.n / kChunk, a.e.dim);
+    const unsigned first = ahead.rows ? grid_of(ahead).x : 0;
+    hipLaunchKernelGGL((rows_kernel<T, TG, FEW, ADD, Q>), dim3(grid_of(p).x + first), dim3(kThreads), 0, stream, a, p, ahead,
+                       static_cast<int>(first), s);
+}
+
+template <class T, class TG, bool FEW> hipError_t backward(const EmbedArgs& a, const OpsDevice& d, hipStream_t stream)
 {
     const Layout l(a.e.count, a.e.vocab, a.e.dim);
     char* scratch = static_cast<char*>(d.scan);
@@ -512,20 +631,34 @@ template <class T, class TG> hipError_t backward(const EmbedArgs& a, const OpsDe
         sort(a, l, scratch, s, stream);
         const Pieces chunks = pieces_of(s.n / kChunk, a.e.dim);
         const int64_t places = over(s.n, kThreads), blocks = grid_of(chunks).x;
-        hipLaunchKernelGGL((chunk_kernel<T>), dim3(static_cast<unsigned>(blocks > places ? blocks : places)), dim3(kThreads), 0, stream,
-                           a, chunks, s);
+        hipLaunchKernelGGL((chunk_kernel<T, FEW>), dim3(static_cast<unsigned>(blocks > places ? blocks : places)), dim3(kThreads), 0,
+                           stream, a, chunks, s);
         if (s.n >= kBigLeast) {
             s.big = reinterpret_cast<float*>(scratch + l.big);
             const Pieces big = pieces_of(s.n / kChunk / kChunk, a.e.dim);
-            hipLaunchKernelGGL(big_chunk_kernel, grid_of(big), dim3(kThreads), 0, stream, a, big, s);
+            hipLaunchKernelGGL((big_chunk_kernel<FEW>), grid_of(big), dim3(kThreads), 0, stream, a, big, s);
         }
     } else if (a.add) {
         return hipSuccess;
     }
-    const Pieces p = pieces_of(a.add ? s.n : a.e.vocab, a.e.dim);
-    if (a.add) hipLaunchKernelGGL((rows_kernel<T, TG, true>), grid_of(p), dim3(kThreads), 0, stream, a, p, s);
-    else hipLaunchKernelGGL((rows_kernel<T, TG, false>), grid_of(p), dim3(kThreads), 0, stream, a, p, s);
+    constexpr int Q = FEW ? 1 : 4;
+    if (FEW || a.e.dim <= 64 * kCols) {
+        if (a.add) rows<T, TG, FEW, true, 1>(a, s, stream);
+        else rows<T, TG, FEW, false, 1>(a, s, stream);
+    } else {
+        if (a.add) rows<T, TG, FEW, true, Q>(a, s, stream);
+        else rows<T, TG, FEW, false, Q>(a, s, stream);
+    }
     return hipGetLastError();
+}
+
+template <class T, class TR> hipError_t forward_of(const EmbedArgs& a, hipStream_t stream)
+{
+    return a.e.dim < kCols ? forward<T, TR, true>(a, stream) : forward<T, TR, false>(a, stream);
+}
+template <class T, class TR> hipError_t backward_of(const EmbedArgs& a, const OpsDevice& d, hipStream_t stream)
+{
+    return a.e.dim < kCols ? backward<TR, T, true>(a, d, stream) : backward<TR, T, false>(a, d, stream);
 }
 
 }  // namespace
@@ -534,13 +667,14 @@ int64_t embed_scratch_bytes(int64_t count, int64_t vocab, int64_t dim) { return 
 
 hipError_t launch_embed_forward(const EmbedArgs& a, bool bf16, bool rows_bf16, hipStream_t stream)
 {
-    return bf16 ? forward<uint16_t>(a, rows_bf16, stream) : forward<float>(a, rows_bf16, stream);
+    if (rows_bf16) return bf16 ? forward_of<uint16_t, uint16_t>(a, stream) : forward_of<float, uint16_t>(a, stream);
+    return bf16 ? forward_of<uint16_t, float>(a, stream) : forward_of<float, float>(a, stream);
 }
 
 hipError_t launch_embed_backward(const EmbedArgs& a, bool bf16, bool rows_bf16, const OpsDevice& d, hipStream_t stream)
 {
-    if (rows_bf16) return bf16 ? backward<uint16_t, uint16_t>(a, d, stream) : backward<uint16_t, float>(a, d, stream);
-    return bf16 ? backward<float, uint16_t>(a, d, stream) : backward<float, float>(a, d, stream);
+    if (rows_bf16) return bf16 ? backward_of<uint16_t, uint16_t>(a, d, stream) : backward_of<float, uint16_t>(a, d, stream);
+    return bf16 ? backward_of<uint16_t, float>(a, d, stream) : backward_of<float, float>(a, d, stream);
 }
 
 }  // namespace gemk

@@ -406,8 +406,8 @@ int gem_copy_f32(const float* src, float* dst, int64_t count, void* stream);
  * What a worker computes from data before it has an update to commit: the
  * scores of a model's logits (a teacher's record, an evaluation), the
  * distillation loss against such a record and the clipped loss of a policy,
- * each with its gradient, an embedding and a gated linear recurrence with
- * their backward passes.  Unlike the commits, which are
+ * each with its gradient, an embedding, a short causal convolution and a gated
+ * linear recurrence with their backward passes.  Unlike the commits, which are
  * held to fixed bits, their values are those of the formulas up to rounding:
  * inputs are binary32 or bfloat16 (GEM_F32, GEM_BF16), sums, states and
  * statistics are binary32, and outputs of the inputs' type are rounded once
@@ -430,6 +430,8 @@ typedef struct gem_ops_handle gem_ops_t;
 #define GEM_TOP_MAX 128
 /* Most tokens of a recurrence. */
 #define GEM_TOKENS_MAX 2147483392
+/* Most taps of a convolution. */
+#define GEM_CONV_MAX 4
 
 /* Create the handle on the current device.  stream is the hipStream_t its work
  * is queued on (NULL: the device's null stream) and must outlive it.
@@ -601,6 +603,53 @@ int gem_embed_scratch(int64_t count, int32_t vocab, int32_t dim, int64_t* bytes)
  * Errors: EINVAL, EDTYPE, EALIGN, ESCRATCH. */
 int gem_embed_backward(gem_ops_t* ops, const gem_embed* e, const void* dout, int64_t dout_stride,
                        int32_t dout_dtype, void* grad, int64_t grad_stride, int32_t add);
+
+/* Inputs of the causal convolution of each channel along its tokens, over
+ * packed sequences as gem_scan has them (offsets, which are read by the
+ * kernels alone; NULL: equal lengths):
+ *     c_t = bias + sum_{j < width} weight[j] x_{t - width + 1 + j}
+ *     y_t = c_t, or with act 1 c_t sigmoid(c_t)
+ * width is 1 to GEM_CONV_MAX, weight [channels][width] and bias [channels]
+ * binary32 (bias NULL: zeros).  Ahead of a sequence stand the width - 1 inputs
+ * of before ([sequences][width - 1][channels] of dtype, earliest first; NULL:
+ * zeros). */
+typedef struct {
+    const void* x;
+    const float* weight;
+    const float* bias;
+    const void* before;
+    const int64_t* offsets;
+    int64_t tokens;
+    int64_t x_stride;
+    int32_t channels;
+    int32_t sequences;
+    int32_t width;
+    int32_t dtype;
+    int32_t act;
+    int32_t reserved;
+} gem_conv;
+
+/* y for every token (dtype).  last (laid out as before; may be NULL) receives the
+ * inputs that stand ahead of each sequence's next token, those of before
+ * among them if it is shorter; it may be before's own memory, so that they are
+ * kept in place: a call with one token a sequence is the answering step.
+ * Errors: EINVAL, EDTYPE, EALIGN. */
+int gem_conv_forward(gem_ops_t* ops, const gem_conv* s, void* y, int64_t y_stride, void* last);
+
+/* Scratch bytes that a gem_ops_t needs for gem_conv_backward of up to these sizes
+ * (smaller ones never need more). */
+int gem_conv_scratch(int64_t tokens, int32_t channels, int64_t* bytes);
+
+/* The backward pass, from dy and dlast (of dtype; dlast NULL: zeros): with g_t =
+ * dy_t times the activation's derivative at c_t, which is formed again,
+ *     dx_t = sum_k weight[width - 1 - k] g_{t + k}  (+ dlast's of that input),
+ *     dweight[j] = sum_t g_t x_{t - width + 1 + j},  dbias = sum_t g_t,
+ * and dbefore the same as dx of the inputs ahead.  dweight, dbias and dbefore
+ * may be NULL.
+ * Errors: EINVAL, EDTYPE, EALIGN, ESCRATCH. */
+int gem_conv_backward(gem_ops_t* ops, const gem_conv* s, const void* dy, int64_t dy_stride,
+                      const void* dlast, void* dx, int64_t dx_stride, float* dweight,
+                      float* dbias, void* dbefore);
 
 /* Inputs of the gated linear recurrence over `sequences` (>= 1) sequences of
  * tokens (0 to GEM_TOKENS_MAX) x channels, packed one after the other:

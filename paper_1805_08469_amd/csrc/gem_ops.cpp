@@ -1,5 +1,6 @@
 // gem_ops.cpp -- the C ABI of the worker's operators: handles and argument
-// checks.  Kernels live in gem_logits.hip, gem_policy.hip, gem_embed.hip and gem_scan.hip.
+// checks.  Kernels live in gem_logits.hip, gem_policy.hip, gem_embed.hip,
+// gem_conv.hip and gem_scan.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -96,6 +97,24 @@ int check_embed(const gem_embed* e, int32_t rows_dtype, const void* rows, int64_
     if (!aligned(e->tokens, 4) || !aligned(rows, element(rows_dtype))) return GEM_EALIGN;
     a->e = *e;
     a->rows = const_cast<void*>(rows);
+    return GEM_OK;
+}
+
+int check_conv(const gem_conv* s, gem_conv* out)
+{
+    if (!s) return GEM_EINVAL;
+    if (s->dtype != GEM_F32 && s->dtype != GEM_BF16) return GEM_EDTYPE;
+    if (s->tokens < 0 || s->tokens > GEM_TOKENS_MAX || s->channels < 1 || s->sequences < 1) return GEM_EINVAL;
+    if (s->width < 1 || s->width > GEM_CONV_MAX || (s->act != 0 && s->act != 1)) return GEM_EINVAL;
+    *out = *s;
+    if (!row_stride(s->x_stride, s->channels, &out->x_stride)) return GEM_EINVAL;
+    if (!s->offsets && s->tokens % s->sequences != 0) return GEM_EINVAL;
+    // A launch's threads, 32 a row, are counted in 32 bits.
+    if (gemk::conv_rows(s->tokens, s->channels) >= int64_t{1} << 27) return GEM_EINVAL;
+    if (!s->weight || (s->tokens > 0 && !s->x)) return GEM_EINVAL;
+    if (!aligned(s->x, element(s->dtype)) || !aligned(s->before, element(s->dtype)) || !aligned(s->weight, 4) ||
+        !aligned(s->bias, 4) || !aligned(s->offsets, 8))
+        return GEM_EALIGN;
     return GEM_OK;
 }
 
@@ -287,6 +306,54 @@ int gem_embed_backward(gem_ops_t* ops, const gem_embed* e, const void* dout, int
     a.add = add != 0;
     if (gemk::embed_scratch_bytes(e->count, e->vocab, e->dim) > ops->dev.scan_bytes) return GEM_ESCRATCH;
     OPS_HIP(gemk::launch_embed_backward(a, e->dtype == GEM_BF16, dout_dtype == GEM_BF16, ops->dev, ops->stream));
+    return GEM_OK;
+}
+
+int gem_conv_forward(gem_ops_t* ops, const gem_conv* s, void* y, int64_t y_stride, void* last)
+{
+    if (!ops) return GEM_EINVAL;
+    gemk::ConvArgs a{};
+    const int rc = check_conv(s, &a.s);
+    if (rc != GEM_OK) return rc;
+    if (s->tokens > 0 && !y) return GEM_EINVAL;
+    if (!row_stride(y_stride, s->channels, &a.y_stride)) return GEM_EINVAL;
+    if (!aligned(y, element(s->dtype)) || !aligned(last, element(s->dtype))) return GEM_EALIGN;
+    a.y = y;
+    a.last = last;
+    OPS_HIP(gemk::launch_conv_forward(a, s->dtype == GEM_BF16, ops->stream));
+    return GEM_OK;
+}
+
+int gem_conv_scratch(int64_t tokens, int32_t channels, int64_t* bytes)
+{
+    if (!bytes || tokens < 0 || tokens > GEM_TOKENS_MAX || channels < 1) return GEM_EINVAL;
+    *bytes = gemk::conv_scratch_bytes(tokens, channels);
+    return GEM_OK;
+}
+
+int gem_conv_backward(gem_ops_t* ops, const gem_conv* s, const void* dy, int64_t dy_stride,
+                      const void* dlast, void* dx, int64_t dx_stride, float* dweight, float* dbias,
+                      void* dbefore)
+{
+    if (!ops) return GEM_EINVAL;
+    gemk::ConvBackArgs a{};
+    const int rc = check_conv(s, &a.s);
+    if (rc != GEM_OK) return rc;
+    if (s->tokens > 0 && (!dy || !dx)) return GEM_EINVAL;
+    if (!row_stride(dy_stride, s->channels, &a.dy_stride)) return GEM_EINVAL;
+    if (!row_stride(dx_stride, s->channels, &a.dx_stride)) return GEM_EINVAL;
+    const size_t e = element(s->dtype);
+    if (!aligned(dy, e) || !aligned(dlast, e) || !aligned(dx, e) || !aligned(dbefore, e) || !aligned(dweight, 4) ||
+        !aligned(dbias, 4))
+        return GEM_EALIGN;
+    a.dy = dy;
+    a.dlast = dlast;
+    a.dx = dx;
+    a.dweight = dweight;
+    a.dbias = dbias;
+    a.dbefore = dbefore;
+    if (gemk::conv_scratch_bytes(s->tokens, s->channels) > ops->dev.scan_bytes) return GEM_ESCRATCH;
+    OPS_HIP(gemk::launch_conv_backward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
 }
 

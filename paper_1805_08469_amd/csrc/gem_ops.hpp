@@ -66,6 +66,25 @@ struct EmbedArgs {
     bool add;
 };
 
+struct ConvArgs {
+    gem_conv s;            // stride filled in
+    void* y;
+    int64_t y_stride;
+    void* last;
+};
+
+struct ConvBackArgs {
+    gem_conv s;
+    const void* dy;
+    int64_t dy_stride;
+    const void* dlast;
+    void* dx;
+    int64_t dx_stride;
+    float* dweight;
+    float* dbias;
+    void* dbefore;
+};
+
 struct ScanArgs {
     gem_scan s;            // strides filled in
     void* y;
@@ -101,6 +120,10 @@ hipError_t launch_policy(const PolicyArgs& a, bool bf16, const OpsDevice& d, hip
 int64_t embed_scratch_bytes(int64_t count, int64_t vocab, int64_t dim);
 hipError_t launch_embed_forward(const EmbedArgs& a, bool bf16, bool rows_bf16, hipStream_t stream);
 hipError_t launch_embed_backward(const EmbedArgs& a, bool bf16, bool rows_bf16, const OpsDevice& d, hipStream_t stream);
+int64_t conv_rows(int64_t tokens, int64_t channels);
+int64_t conv_scratch_bytes(int64_t tokens, int64_t channels);
+hipError_t launch_conv_forward(const ConvArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_conv_backward(const ConvBackArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 int64_t scan_rows(int64_t tokens, int64_t channels);
 int64_t scan_bytes(int64_t tokens, int64_t channels);            // of a launch
 int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);    // of it and of any smaller one

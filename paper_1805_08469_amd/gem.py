@@ -42,6 +42,7 @@ GEM_PI_BINS = 643
 GEM_VOCAB_MAX = 1 << 22
 GEM_TOP_MAX = 128
 GEM_TOKENS_MAX = (1 << 31) - 256
+GEM_CONV_MAX = 4
 
 # Every symbol include/gem.h declares.
 EXPORTED = (
@@ -54,7 +55,8 @@ EXPORTED = (
     "gem_set_cache_policy", "gem_dims", "gem_gather_static",
     "gem_ops_create", "gem_ops_destroy", "gem_token_scores", "gem_distill_loss",
     "gem_distill_grad", "gem_policy_loss", "gem_policy_grad", "gem_embed_forward",
-    "gem_embed_scratch", "gem_embed_backward", "gem_scan_scratch", "gem_scan_state_rows",
+    "gem_embed_scratch", "gem_embed_backward", "gem_conv_forward", "gem_conv_scratch",
+    "gem_conv_backward", "gem_scan_scratch", "gem_scan_state_rows",
     "gem_scan_forward", "gem_scan_backward",
 )
 
@@ -115,6 +117,14 @@ class gem_embed(C.Structure):
     _fields_ = [("table", C.c_void_p), ("tokens", C.c_void_p), ("count", C.c_int64),
                 ("stride", C.c_int64), ("vocab", C.c_int32), ("dim", C.c_int32),
                 ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
+class gem_conv(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("before", C.c_void_p), ("offsets", C.c_void_p), ("tokens", C.c_int64),
+                ("x_stride", C.c_int64), ("channels", C.c_int32), ("sequences", C.c_int32),
+                ("width", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 class gem_scan(C.Structure):
@@ -197,6 +207,10 @@ def _load():
         "gem_embed_scratch": (C.c_int, [C.c_int64, C.c_int32, C.c_int32, i64p]),
         "gem_embed_backward": (C.c_int, [vp, C.POINTER(gem_embed), vp, C.c_int64, C.c_int32, vp,
                                          C.c_int64, C.c_int32]),
+        "gem_conv_forward": (C.c_int, [vp, C.POINTER(gem_conv), vp, C.c_int64, vp]),
+        "gem_conv_scratch": (C.c_int, [C.c_int64, C.c_int32, i64p]),
+        "gem_conv_backward": (C.c_int, [vp, C.POINTER(gem_conv), vp, C.c_int64, vp, vp, C.c_int64,
+                                        vp, vp, vp]),
         "gem_scan_scratch": (C.c_int, [C.c_int64, C.c_int32, i64p]),
         "gem_scan_state_rows": (C.c_int, [C.c_int64, i64p]),
         "gem_scan_forward": (C.c_int, [vp, C.POINTER(gem_scan), vp, C.c_int64, vp, vp]),
@@ -508,6 +522,22 @@ def gem_embed_backward(ops: int, e: gem_embed, dout: int, dout_stride: int, dout
                                  add), "gem_embed_backward")
 
 
+def gem_conv_forward(ops: int, s: gem_conv, y: int, y_stride: int, last: int) -> None:
+    _check(_L.gem_conv_forward(ops, C.byref(s), y, y_stride, last), "gem_conv_forward")
+
+
+def gem_conv_scratch(tokens: int, channels: int) -> int:
+    out = C.c_int64()
+    _check(_L.gem_conv_scratch(tokens, channels, C.byref(out)), "gem_conv_scratch")
+    return out.value
+
+
+def gem_conv_backward(ops: int, s: gem_conv, dy: int, dy_stride: int, dlast: int, dx: int,
+                      dx_stride: int, dweight: int, dbias: int, dbefore: int) -> None:
+    _check(_L.gem_conv_backward(ops, C.byref(s), dy, dy_stride, dlast, dx, dx_stride, dweight,
+                                dbias, dbefore), "gem_conv_backward")
+
+
 def gem_scan_scratch(tokens: int, channels: int) -> int:
     out = C.c_int64()
     _check(_L.gem_scan_scratch(tokens, channels, C.byref(out)), "gem_scan_scratch")
@@ -669,6 +699,19 @@ class Ops:
                        dout_stride=0, grad_stride=0, add=0):
         gem_embed_backward(self.h, gem_embed(None, tokens, count, 0, vocab, dim, dtype, scale),
                            dout, dout_stride, dout_dtype, grad, grad_stride, add)
+
+    def conv_forward(self, x, weight, tokens, channels, sequences, width, dtype, y, bias=None,
+                     before=None, last=None, offsets=None, act=0, x_stride=0, y_stride=0):
+        s = gem_conv(x, weight, bias, before, offsets, tokens, x_stride, channels, sequences, width,
+                     dtype, act, 0)
+        gem_conv_forward(self.h, s, y, y_stride, last)
+
+    def conv_backward(self, x, weight, tokens, channels, sequences, width, dtype, dy, dx,
+                      dweight=None, bias=None, dbias=None, before=None, dbefore=None, dlast=None,
+                      offsets=None, act=0, x_stride=0, dy_stride=0, dx_stride=0):
+        s = gem_conv(x, weight, bias, before, offsets, tokens, x_stride, channels, sequences, width,
+                     dtype, act, 0)
+        gem_conv_backward(self.h, s, dy, dy_stride, dlast, dx, dx_stride, dweight, dbias, dbefore)
 
     def scan_forward(self, x, gate, tokens, channels, sequences, dtype, y, offsets=None, h0=None,
                      h_last=None, states=None, x_stride=0, gate_stride=0, y_stride=0):

@@ -1,0 +1,310 @@
+"""The causal convolution and its backward pass against their definition in 64 bits."""
+import pytest
+import torch
+
+from paper_1805_08469_amd import gem as G
+
+U = 2.0 ** -24
+HALF = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
+KIND = {torch.float32: G.GEM_F32, torch.bfloat16: G.GEM_BF16}
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def reference(x, w, bias, before, off, act, dy=None, dlast=None):
+    """Values, and bounds: a token's sum is off by W + 2 roundings of its terms' sizes (c_e), its sigmoid
+    by 8 + 2 |c|, and silu has slopes of at most 1.1 and curvatures of at most 0.5."""
+    D, W = w.shape
+    x, w, before = x.double().requires_grad_(), w.double().requires_grad_(), before.double().requires_grad_()
+    bias = bias.double().requires_grad_()
+    seqs = [(torch.cat([before[q], x[a:b]]), b - a) for q, (a, b) in enumerate(zip(off, off[1:]))]
+    c = torch.cat([sum(e[j:j + n] * w[:, j] for j in range(W)) + bias for e, n in seqs])
+    y = torch.nn.functional.silu(c) if act else c
+    last = torch.stack([e[n:] for e, n in seqs])
+    with torch.no_grad():
+        c_e = U * (W + 2) * (torch.cat([sum((e[j:j + n] * w[:, j]).abs() for j in range(W)) for e, n in seqs]) + bias.abs())
+        rel = U * (8 + 2 * c.abs())
+        y_e = 1.1 * c_e + rel * y.abs() if act else c_e
+        r = dict(y=(y, y_e), last=(last, 0 * last))
+    if dy is None:
+        return {n: (v.detach(), e) for n, (v, e) in r.items()}
+    total = (y * dy.double()).sum() + (last * dlast.double()).sum()
+    dx, dw, db, dbefore = torch.autograd.grad(total, [x, w, bias, before])
+    with torch.no_grad():
+        s = torch.sigmoid(c)
+        slope = s + c * s * (1 - s) if act else torch.ones_like(c)
+        g = dy.double() * slope
+        g_e = dy.double().abs() * (0.5 * c_e + 3 * rel * (s + c.abs() * s * (1 - s))) if act else 0 * g
+        n = sum(b - a for a, b in zip(off, off[1:]))
+        dx_e, dw_e, dbefore_e = torch.zeros_like(x), torch.zeros_like(w), torch.zeros_like(before)
+        for q, (a, b) in enumerate(zip(off, off[1:])):
+            e = seqs[q][0].abs()
+            ext = torch.zeros_like(e)
+            for j in range(W):
+                ext[j:j + b - a] += w[:, j].abs() * (g_e[a:b] + U * (W + 2) * g[a:b].abs())
+                dw_e[:, j] += (e[j:j + b - a] * (g_e[a:b] + U * (160 + n / 64) * g[a:b].abs())).sum(0)
+            ext[b - a:] += 2 * U * dlast[q].double().abs()
+            dbefore_e[q], dx_e[a:b] = ext[:W - 1], ext[W - 1:]
+        db_e = (g_e + U * (160 + n / 64) * g.abs()).sum(0)
+    r.update(dx=(dx, dx_e), dweight=(dw, dw_e), dbias=(db, db_e), dbefore=(dbefore, dbefore_e))
+    return {n: (v.detach(), e) for n, (v, e) in r.items()}
+
+
+def off(got, want):
+    v, e = want
+    return ((got.double() - v).abs() - e - v.abs() * HALF[got.dtype] - 1e-37).max().item() if v.numel() else -1.0
+
+
+def cuts(kind, tokens, seqs, g):
+    if kind == "equal":
+        return [tokens // seqs * i for i in range(seqs + 1)]
+    c = sorted(int(v) for v in torch.randint(tokens + 1, (seqs - 1,), generator=g))
+    if seqs > 4:
+        c[1] = c[0]                       # empty, and short ones next to each other
+        c[3] = min(c[2] + 1, tokens)
+        c.sort()
+    return [0] + c + [tokens]
+
+
+def wide(rows, cols, pad, dtype, g=None):
+    t = torch.full((rows, cols + pad), 7.0, device="cuda", dtype=dtype)
+    if g is not None:
+        t[:, :cols] = torch.randn(rows, cols, generator=g).cuda()
+    return t
+
+
+def make(tokens, seqs, D, W, dtype, pad, kind, seed=0):
+    g = torch.Generator().manual_seed(seed + tokens)
+    s = dict(x=wide(tokens, D, pad, dtype, g), dy=wide(tokens, D, pad, dtype, g), y=wide(tokens, D, pad, dtype),
+             dx=wide(tokens, D, pad, dtype), w=torch.randn(D, W, generator=g).cuda(), b=torch.randn(D, generator=g).cuda())
+    for n in ("before", "dlast"):
+        s[n] = torch.randn(seqs, W - 1, D, generator=g).cuda().to(dtype)
+    s.update(last=torch.full_like(s["before"], 7), dbefore=torch.full_like(s["before"], 7), dw=torch.full_like(s["w"], 7),
+             db=torch.full_like(s["b"], 7), off=cuts(kind, tokens, seqs, g))
+    s["offsets"] = torch.tensor(s["off"], device="cuda") if kind != "equal" else None
+    return s
+
+
+def ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def forward(ops, s, D, W, act, last="last", before="before", bias=True):
+    n, seqs = s["x"].shape[0], len(s["off"]) - 1
+    ops.conv_forward(s["x"].data_ptr(), s["w"].data_ptr(), n, D, seqs, W, KIND[s["x"].dtype], y=s["y"].data_ptr(),
+                     bias=ptr(s["b"]) if bias else None, before=ptr(s.get(before)), last=ptr(s.get(last)),
+                     offsets=ptr(s["offsets"]), act=act, x_stride=s["x"].stride(0), y_stride=s["y"].stride(0))
+
+
+def backward(ops, s, D, W, act, dlast="dlast"):
+    n, seqs = s["x"].shape[0], len(s["off"]) - 1
+    ops.conv_backward(s["x"].data_ptr(), s["w"].data_ptr(), n, D, seqs, W, KIND[s["x"].dtype], dy=s["dy"].data_ptr(),
+                      dx=s["dx"].data_ptr(), dweight=s["dw"].data_ptr(), bias=ptr(s["b"]), dbias=s["db"].data_ptr(),
+                      before=ptr(s["before"]), dbefore=ptr(s["dbefore"]), dlast=ptr(s.get(dlast)), offsets=ptr(s["offsets"]),
+                      act=act, x_stride=s["x"].stride(0), dy_stride=s["dy"].stride(0), dx_stride=s["dx"].stride(0))
+
+
+def ops_for(tokens, D, stream=None):
+    return G.Ops(G.gem_conv_scratch(tokens, D), stream or torch.cuda.current_stream().cuda_stream)
+
+
+CASES = [(1, 1, 1), (5, 1, 3), (7, 7, 130), (8, 1, 2), (40, 5, 64), (64, 16, 129), (257, 9, 66), (1000, 8, 200),
+         (1000, 1, 515), (4099, 30, 33), (30000, 12, 128)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("W", [1, 2, 3, 4])
+@pytest.mark.parametrize("tokens,seqs,D", CASES)
+def test_forward_and_backward(tokens, seqs, D, W, dtype):
+    """Equal and ragged sequences, among them empty ones and some shorter than the taps."""
+    for kind, pad, act in (("equal", 0, 1), ("ragged", 3, 1), ("ragged", 0, 0)):
+        if kind == "equal" and tokens % seqs:
+            continue
+        s = make(tokens, seqs, D, W, dtype, pad, kind)
+        dlast = "dlast" if act else "none"
+        with ops_for(tokens, D) as ops:
+            forward(ops, s, D, W, act)
+            backward(ops, s, D, W, act, dlast)
+            want = reference(s["x"][:, :D], s["w"], s["b"], s["before"], s["off"], act, s["dy"][:, :D],
+                             s["dlast"] if act else torch.zeros_like(s["dlast"]))
+            for n, got in dict(y=s["y"][:, :D], last=s["last"], dx=s["dx"][:, :D], dweight=s["dw"], dbias=s["db"],
+                               dbefore=s["dbefore"]).items():
+                assert off(got, want[n]) <= 0, (kind, n, off(got, want[n]))
+            if pad:
+                assert (s["y"][:, D:] == 7).all() and (s["dx"][:, D:] == 7).all()
+            first = {n: s[n].clone() for n in ("y", "last", "dx", "dw", "db", "dbefore")}
+            forward(ops, s, D, W, act)
+            backward(ops, s, D, W, act, dlast)
+            assert all(torch.equal(first[n], s[n]) for n in first)
+            forward(ops, s, D, W, act, last="before")        # kept in place
+            assert torch.equal(s["before"], first["last"]) and torch.equal(s["y"], first["y"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [1, 130, 1001])
+def test_tokens_one_at_a_time_are_a_sequence(D, dtype):
+    """Answers from inputs kept in place, against the whole sequences' call: the same bits."""
+    seqs, n, W = 5, 9, 4
+    s = make(seqs * n, seqs, D, W, dtype, 0, "equal")
+    with ops_for(seqs * n, D) as ops:
+        forward(ops, s, D, W, 1)
+        x, y, last = s["x"].view(seqs, n, D), s["y"].clone().view(seqs, n, D), s["last"].clone()
+        for t in range(n):
+            one = dict(s, x=x[:, t].contiguous(), y=torch.empty(seqs, D, device="cuda", dtype=dtype), off=list(range(seqs + 1)))
+            forward(ops, one, D, W, 1, last="before")
+            assert torch.equal(one["y"], y[:, t])
+        assert torch.equal(s["before"], last)
+
+
+@pytest.mark.gpu
+def test_left_out():
+    """No bias, nothing ahead, no tokens; what is not asked for."""
+    s = make(50, 3, 20, 4, F32, 0, "ragged")
+    with ops_for(50, 20) as ops:
+        forward(ops, s, 20, 4, 1, last="none", before="none", bias=False)
+        want = reference(s["x"], s["w"], torch.zeros_like(s["b"]), torch.zeros_like(s["before"]), s["off"], 1)
+        assert off(s["y"], want["y"]) <= 0 and (s["last"] == 7).all()
+        e = make(0, 3, 20, 4, F32, 0, "equal")
+        forward(ops, e, 20, 4, 1)
+        assert torch.equal(e["last"], e["before"])
+        backward(ops, e, 20, 4, 1)
+        assert (e["dw"] == 0).all() and (e["db"] == 0).all() and torch.equal(e["dbefore"], e["dlast"])
+
+
+@pytest.mark.gpu
+def test_nothing_passes_between_sequences():
+    """No numbers in one sequence, and in what is ahead of it, leave the others as they are."""
+    s = make(200, 6, 70, 4, F32, 0, "ragged", seed=3)
+    with ops_for(200, 70) as ops:
+        forward(ops, s, 70, 4, 1)
+        backward(ops, s, 70, 4, 1)
+        first = {n: s[n].clone() for n in ("y", "dx", "last", "dbefore")}
+        for q, (a, b) in enumerate(zip(s["off"], s["off"][1:])):
+            if b > a:
+                break
+        s["x"][a:b], s["before"][q], s["dy"][a:b] = float("nan"), float("inf"), float("nan")
+        forward(ops, s, 70, 4, 1)
+        backward(ops, s, 70, 4, 1)
+    rest, others = [t for t in range(200) if not a <= t < b], [k for k in range(6) if k != q]
+    for n in ("y", "dx"):
+        assert torch.equal(s[n][rest], first[n][rest]) and s[n][a:b].isnan().any()
+    for n in ("last", "dbefore"):
+        assert torch.equal(s[n][others], first[n][others])
+
+
+@pytest.mark.gpu
+def test_offsets_of_any_values_stay_in_the_arrays():
+    """They are not checked on the host; every array ends where another that is watched begins."""
+    n, seqs, D, W = 60, 5, 33, 4
+    for bad in ([0, 70, 10, -5, 900, 60], [5, 4, 3, 2, 1, 0], [0, 0, 0, 0, 0, 0], [60] * 6, [-2 ** 62, 2 ** 62, 3, 3, 40, 2 ** 40],
+                [10, 20, 30, 40, 50, 55]):
+        s = make(n, seqs, D, W, F32, 0, "ragged")
+        names = ("y", "dx", "last", "dbefore")
+        room = {k: torch.full((3 * s[k].numel(),), 7.0, device="cuda") for k in names}
+        for k in names:
+            s[k] = room[k][s[k].numel():2 * s[k].numel()].view(s[k].shape)
+        s["offsets"] = torch.tensor(bad, device="cuda")
+        with ops_for(n, D) as ops:
+            forward(ops, s, D, W, 1)
+            backward(ops, s, D, W, 1)
+        torch.cuda.synchronize()
+        for k in names:
+            m = s[k].numel()
+            assert (room[k][:m] == 7).all() and (room[k][2 * m:] == 7).all(), (bad, k)
+
+
+@pytest.mark.gpu
+def test_same_bits_on_a_stream_and_in_graphs():
+    s = torch.cuda.Stream()
+    sets = [make(3000 + 100 * i, 4, 260, 4, BF16, 0, "equal", seed=i) for i in range(2)]
+    torch.cuda.synchronize()
+    with ops_for(3100, 260, s.cuda_stream) as ops:
+        want, graphs = [], []
+        for v in sets:
+            forward(ops, v, 260, 4, 1)
+            backward(ops, v, 260, 4, 1)
+            s.synchronize()
+            want.append({n: v[n].clone() for n in ("y", "last", "dx", "dw", "db", "dbefore")})
+        for v in sets:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                forward(ops, v, 260, 4, 1)
+                backward(ops, v, 260, 4, 1)
+            graphs.append(graph)
+        for _ in range(3):
+            for v, graph, w in zip(sets, graphs, want):
+                for n in w:
+                    v[n].fill_(5)
+                torch.cuda.synchronize()
+                with torch.cuda.stream(s):
+                    graph.replay()
+                s.synchronize()
+                assert all(torch.equal(v[n], w[n]) for n in w)
+        del graphs
+
+
+@pytest.mark.gpu
+def test_more_elements_than_32_bits_count():
+    n, D = 1050000, 2056
+    x = torch.zeros(n, D, device="cuda", dtype=BF16)
+    x[-3] = 1.0
+    w = torch.tensor([[4.0, 3.0, 2.0, 1.0]], device="cuda").repeat(D, 1)
+    y = torch.empty_like(x)
+    with G.Ops(0, torch.cuda.current_stream().cuda_stream) as ops:
+        ops.conv_forward(x.data_ptr(), w.data_ptr(), n, D, 1, 4, 1, y=y.data_ptr())
+        assert (y[-3:, 0].tolist(), y[-3:, -1].tolist()) == ([1.0, 2.0, 3.0], [1.0, 2.0, 3.0])
+        assert int(y.count_nonzero()) == 3 * D
+
+
+@pytest.mark.parametrize("channels", [1, 64, 65, 128, 129, 1001, 2048, 8192, 600000])
+def test_scratch_holds_every_shorter_batch(channels):
+    """Five sums a channel of each run, whose length is halved from 128 to 16 tokens until they leave
+    4096 rows of 128 channels."""
+    def taken(tokens):
+        length = 128
+        while length > 16 and -(-tokens // length) * -(-channels // 128) < 4096:
+            length //= 2
+        return 20 * channels * -(-tokens // length)
+
+    worst, before = 0, 0
+    for tokens in list(range(0, 140000, 31)) + [2 ** 20, 2 ** 24 + 1]:
+        worst, now = max(worst, taken(tokens)), G.gem_conv_scratch(tokens, channels)
+        assert now >= worst and now >= before, tokens
+        assert G.gem_conv_scratch(tokens, channels + 1) >= now
+        before = now
+
+
+def test_refusals():
+    """On the host, before any work is queued."""
+    L, C, n = G.lib(), G.C, G.C.c_int64()
+    fake = 1 << 20
+
+    def conv(**k):
+        d = dict(x=64, weight=64, bias=None, before=None, offsets=None, tokens=4, x_stride=0, channels=8, sequences=2, width=4,
+                 dtype=0, act=0, reserved=0)
+        d.update(k)
+        return G.gem_conv(*d.values())
+
+    def forward(y=64, stride=0, last=None, ops=fake, **k):
+        s = conv(**k)
+        return L.gem_conv_forward(ops, C.byref(s), y, stride, last)
+
+    def backward(dy=64, dy_stride=0, dlast=None, dx=64, dx_stride=0, dw=64, db=64, dbefore=None, ops=fake, **k):
+        s = conv(**k)
+        return L.gem_conv_backward(ops, C.byref(s), dy, dy_stride, dlast, dx, dx_stride, dw, db, dbefore)
+
+    assert L.gem_conv_forward(fake, None, 64, 0, None) == G.GEM_EINVAL
+    for f in (forward, backward):
+        for k in (dict(ops=None), dict(x=None), dict(weight=None), dict(tokens=-2), dict(tokens=3), dict(channels=0), dict(sequences=0),
+                  dict(width=0), dict(width=5), dict(act=2), dict(x_stride=7), dict(tokens=G.GEM_TOKENS_MAX + 1, sequences=1),
+                  dict(tokens=2 ** 30, channels=2 ** 27, sequences=1)):
+            assert f(**k) == G.GEM_EINVAL, k
+        assert f(dtype=7) == G.GEM_EDTYPE
+        for k in ("x", "weight", "bias", "before", "offsets"):
+            assert f(**{k: 66}) == G.GEM_EALIGN, k
+    assert forward(y=None) == forward(stride=7) == backward(dy=None) == backward(dx=None) == backward(dy_stride=7) == G.GEM_EINVAL
+    assert forward(last=66) == forward(y=66) == G.GEM_EALIGN
+    for k in ("dy", "dlast", "dx", "dw", "db", "dbefore"):
+        assert backward(**{k: 66}) == G.GEM_EALIGN, k
+    assert L.gem_conv_scratch(-1, 1, C.byref(n)) == L.gem_conv_scratch(1, 0, C.byref(n)) == L.gem_conv_scratch(1, 1, None) == G.GEM_EINVAL

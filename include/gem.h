@@ -406,8 +406,8 @@ int gem_copy_f32(const float* src, float* dst, int64_t count, void* stream);
  * What a worker computes from data before it has an update to commit: the
  * scores of a model's logits (a teacher's record, an evaluation), the
  * distillation loss against such a record and the clipped loss of a policy,
- * each with its gradient, an embedding, a short causal convolution and a gated
- * linear recurrence with their backward passes.  Unlike the commits, which are
+ * each with its gradient, an embedding, a short causal convolution, a selective
+ * state space scan and a gated linear recurrence with their backward passes.  Unlike the commits, which are
  * held to fixed bits, their values are those of the formulas up to rounding:
  * inputs are binary32 or bfloat16 (GEM_F32, GEM_BF16), sums, states and
  * statistics are binary32, and outputs of the inputs' type are rounded once
@@ -432,6 +432,8 @@ typedef struct gem_ops_handle gem_ops_t;
 #define GEM_TOKENS_MAX 2147483392
 /* Most taps of a convolution. */
 #define GEM_CONV_MAX 4
+/* Most states of a channel of the selective scan. */
+#define GEM_STATE_MAX 16
 
 /* Create the handle on the current device.  stream is the hipStream_t its work
  * is queued on (NULL: the device's null stream) and must outlive it.
@@ -650,6 +652,93 @@ int gem_conv_scratch(int64_t tokens, int32_t channels, int64_t* bytes);
 int gem_conv_backward(gem_ops_t* ops, const gem_conv* s, const void* dy, int64_t dy_stride,
                       const void* dlast, void* dx, int64_t dx_stride, float* dweight,
                       float* dbias, void* dbefore);
+
+/* Inputs of the selective state space scan over packed sequences as gem_scan has
+ * them (offsets, which are read by the kernels alone; NULL: equal lengths).  For
+ * each channel, with `state` states n (1 to GEM_STATE_MAX; channels x state at
+ * most 2^27),
+ *     u_t = softplus(dt_t + dt_bias)
+ *     h_t[n] = exp(u_t a[n]) h_{t-1}[n] + u_t b_t[n] x_t
+ *     y_t = (sum_n c_t[n] h_t[n] + d x_t) [silu(z_t)]
+ * x, dt and z are tokens x channels, b and c tokens x state and shared by all
+ * channels (dtype); a is [channels][state] (negative where states decay), d and
+ * dt_bias [channels], h0 [sequences][channels][state], binary32.  z NULL: no
+ * gate; d, dt_bias, h0 NULL: zeros. */
+typedef struct {
+    const void* x;
+    const void* dt;
+    const void* b;
+    const void* c;
+    const void* z;
+    const float* a;
+    const float* d;
+    const float* dt_bias;
+    const float* h0;
+    const int64_t* offsets;
+    int64_t tokens;
+    int64_t x_stride;
+    int64_t dt_stride;
+    int64_t b_stride;
+    int64_t c_stride;
+    int64_t z_stride;
+    int32_t channels;
+    int32_t state;
+    int32_t sequences;
+    int32_t dtype;
+} gem_ssm;
+
+/* Scratch bytes that a gem_ops_t needs for scans of up to these sizes (the same for
+ * both directions; smaller ones never need more; a call with one token a sequence
+ * and no offsets needs none), and the rows of the states that forward keeps for
+ * backward. */
+int gem_ssm_scratch(int64_t tokens, int32_t channels, int32_t state, int64_t* bytes);
+int gem_ssm_state_rows(int64_t tokens, int64_t* rows);
+
+/* y for every token (dtype), and h_last (laid out as h0; may be NULL) after each
+ * sequence's last (h0 for an empty one).  h_last may be h0's own memory, so that
+ * a state is kept in place: a call with one token a sequence is the answering
+ * step.  states, if not NULL, receives gem_ssm_state_rows(tokens) rows of
+ * channels x state binary32 values for gem_ssm_backward.
+ * Errors: EINVAL, EDTYPE, EALIGN, ESCRATCH. */
+int gem_ssm_forward(gem_ops_t* ops, const gem_ssm* s, void* y, int64_t y_stride, float* h_last,
+                    float* states);
+
+/* Of the backward pass: dy (dtype) and dh_last (laid out as h0; NULL: zeros), and
+ * the gradients of the inputs by their names and types.  dz, da, dd, ddt_bias
+ * and dh0 may be NULL. */
+typedef struct {
+    const void* dy;
+    const float* dh_last;
+    void* dx;
+    void* ddt;
+    void* db;
+    void* dc;
+    void* dz;
+    float* da;
+    float* dd;
+    float* ddt_bias;
+    float* dh0;
+    int64_t dy_stride;
+    int64_t dx_stride;
+    int64_t ddt_stride;
+    int64_t db_stride;
+    int64_t dc_stride;
+    int64_t dz_stride;
+} gem_ssm_grad;
+
+/* The backward pass, with the states of the forward call on the same inputs: with
+ * g_t = dy_t [silu(z_t)] and r_t[n] = c_t[n] g_t + exp(u_{t+1} a[n]) r_{t+1}[n] (dh_last in
+ * place of the last at a sequence's end), p_t[n] = r_t[n] exp(u_t a[n]) h_{t-1}[n],
+ *     dx_t = d g_t + u_t sum_n r_t[n] b_t[n]
+ *     ddt_t = (x_t sum_n r_t[n] b_t[n] + sum_n p_t[n] a[n]) sigmoid(dt_t + dt_bias)
+ *     dz_t = dy_t (sum_n c_t[n] h_t[n] + d x_t) silu'(z_t)
+ *     db_t[n] = sum over channels of u_t x_t r_t[n],  dc_t[n] = of g_t h_t[n]
+ *     da[n] = sum_t u_t p_t[n],  dd = sum_t g_t x_t,  ddt_bias = sum_t ddt_t
+ *     dh0[n] = exp(u_0 a[n]) r_0[n]  (dh_last for an empty sequence).
+ * h is formed again in binary32 from the states.
+ * Errors: EINVAL, EDTYPE, EALIGN, ESCRATCH. */
+int gem_ssm_backward(gem_ops_t* ops, const gem_ssm* s, const float* states,
+                     const gem_ssm_grad* g);
 
 /* Inputs of the gated linear recurrence over `sequences` (>= 1) sequences of
  * tokens (0 to GEM_TOKENS_MAX) x channels, packed one after the other:

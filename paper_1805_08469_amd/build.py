@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgem.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("gem_kernels.hip", "gem_api.cpp", "gem_logits.hip",
                                             "gem_policy.hip", "gem_embed.hip", "gem_conv.hip",
-                                            "gem_scan.hip", "gem_ops.cpp")]
+                                            "gem_ssm.hip", "gem_scan.hip", "gem_ops.cpp")]
 # Device self-tests of the numerics (used by the test suite only).
 SELFTEST_LIB = os.path.join(HERE, "libgem_selftest.so")
 SELFTEST_SOURCES = [os.path.join(CSRC, "gem_selftest.hip")]

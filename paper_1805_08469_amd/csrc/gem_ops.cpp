@@ -1,6 +1,6 @@
 // gem_ops.cpp -- the C ABI of the worker's operators: handles and argument
 // checks.  Kernels live in gem_logits.hip, gem_policy.hip, gem_embed.hip,
-// gem_conv.hip and gem_scan.hip.
+// gem_conv.hip, gem_ssm.hip and gem_scan.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -30,6 +30,9 @@ namespace {
 // GEM_TOKENS_MAX and of elements' sizes stay within 63 bits.
 constexpr int64_t kRowsMax = int64_t{1} << 22;
 constexpr int64_t kStrideMax = int64_t{1} << 28;
+
+// Most channels x states of a selective scan (a launch has sixteen threads for each).
+constexpr int64_t kChainsMost = int64_t{1} << 27;
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -116,6 +119,33 @@ int check_conv(const gem_conv* s, gem_conv* out)
         !aligned(s->bias, 4) || !aligned(s->offsets, 8))
         return GEM_EALIGN;
     return GEM_OK;
+}
+
+int check_ssm(const gem_ssm* s, gem_ssm* out)
+{
+    if (!s) return GEM_EINVAL;
+    if (s->dtype != GEM_F32 && s->dtype != GEM_BF16) return GEM_EDTYPE;
+    if (s->tokens < 0 || s->tokens > GEM_TOKENS_MAX || s->channels < 1 || s->sequences < 1) return GEM_EINVAL;
+    if (s->state < 1 || s->state > GEM_STATE_MAX || int64_t{s->channels} * s->state > kChainsMost) return GEM_EINVAL;
+    *out = *s;
+    if (!row_stride(s->x_stride, s->channels, &out->x_stride) || !row_stride(s->dt_stride, s->channels, &out->dt_stride) ||
+        !row_stride(s->z_stride, s->channels, &out->z_stride) || !row_stride(s->b_stride, s->state, &out->b_stride) ||
+        !row_stride(s->c_stride, s->state, &out->c_stride))
+        return GEM_EINVAL;
+    if (!s->offsets && s->tokens % s->sequences != 0) return GEM_EINVAL;
+    // A launch's threads, 64 a row, are counted in 32 bits.
+    if (gemk::ssm_rows(s->tokens, s->sequences, s->offsets != nullptr, s->channels) >= int64_t{1} << 26) return GEM_EINVAL;
+    if (!s->a || (s->tokens > 0 && (!s->x || !s->dt || !s->b || !s->c))) return GEM_EINVAL;
+    const size_t e = element(s->dtype);
+    if (!aligned(s->x, e) || !aligned(s->dt, e) || !aligned(s->b, e) || !aligned(s->c, e) || !aligned(s->z, e) ||
+        !aligned(s->a, 4) || !aligned(s->d, 4) || !aligned(s->dt_bias, 4) || !aligned(s->h0, 4) || !aligned(s->offsets, 8))
+        return GEM_EALIGN;
+    return GEM_OK;
+}
+
+bool ssm_fits(const gem_ssm& s, bool back, const gemk::OpsDevice& d)
+{
+    return gemk::ssm_bytes(s.tokens, s.sequences, s.offsets != nullptr, s.channels, s.state, back) <= d.scan_bytes;
 }
 
 // One token a sequence needs no scratch.
@@ -354,6 +384,58 @@ int gem_conv_backward(gem_ops_t* ops, const gem_conv* s, const void* dy, int64_t
     a.dbefore = dbefore;
     if (gemk::conv_scratch_bytes(s->tokens, s->channels) > ops->dev.scan_bytes) return GEM_ESCRATCH;
     OPS_HIP(gemk::launch_conv_backward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
+    return GEM_OK;
+}
+
+int gem_ssm_scratch(int64_t tokens, int32_t channels, int32_t state, int64_t* bytes)
+{
+    if (!bytes || tokens < 0 || tokens > GEM_TOKENS_MAX || channels < 1 || state < 1 || state > GEM_STATE_MAX ||
+        int64_t{channels} * state > kChainsMost)
+        return GEM_EINVAL;
+    *bytes = gemk::ssm_scratch_bytes(tokens, channels, state);
+    return GEM_OK;
+}
+
+int gem_ssm_state_rows(int64_t tokens, int64_t* rows) { return gem_scan_state_rows(tokens, rows); }
+
+int gem_ssm_forward(gem_ops_t* ops, const gem_ssm* s, void* y, int64_t y_stride, float* h_last, float* states)
+{
+    if (!ops) return GEM_EINVAL;
+    gemk::SsmArgs a{};
+    const int rc = check_ssm(s, &a.s);
+    if (rc != GEM_OK) return rc;
+    if (s->tokens > 0 && !y) return GEM_EINVAL;
+    if (!row_stride(y_stride, s->channels, &a.y_stride)) return GEM_EINVAL;
+    if (!aligned(y, element(s->dtype)) || !aligned(h_last, 4) || !aligned(states, 4)) return GEM_EALIGN;
+    a.y = y;
+    a.h_last = h_last;
+    a.states = states;
+    if (!ssm_fits(*s, false, ops->dev)) return GEM_ESCRATCH;
+    OPS_HIP(gemk::launch_ssm_forward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
+    return GEM_OK;
+}
+
+int gem_ssm_backward(gem_ops_t* ops, const gem_ssm* s, const float* states, const gem_ssm_grad* g)
+{
+    if (!ops || !g) return GEM_EINVAL;
+    gemk::SsmBackArgs a{};
+    const int rc = check_ssm(s, &a.s);
+    if (rc != GEM_OK) return rc;
+    if (s->tokens > 0 && (!states || !g->dy || !g->dx || !g->ddt || !g->db || !g->dc)) return GEM_EINVAL;
+    if (g->dz && !s->z) return GEM_EINVAL;
+    a.g = *g;
+    if (!row_stride(g->dy_stride, s->channels, &a.g.dy_stride) || !row_stride(g->dx_stride, s->channels, &a.g.dx_stride) ||
+        !row_stride(g->ddt_stride, s->channels, &a.g.ddt_stride) || !row_stride(g->dz_stride, s->channels, &a.g.dz_stride) ||
+        !row_stride(g->db_stride, s->state, &a.g.db_stride) || !row_stride(g->dc_stride, s->state, &a.g.dc_stride))
+        return GEM_EINVAL;
+    const size_t e = element(s->dtype);
+    if (!aligned(g->dy, e) || !aligned(g->dx, e) || !aligned(g->ddt, e) || !aligned(g->db, e) || !aligned(g->dc, e) ||
+        !aligned(g->dz, e) || !aligned(states, 4) || !aligned(g->dh_last, 4) || !aligned(g->da, 4) || !aligned(g->dd, 4) ||
+        !aligned(g->ddt_bias, 4) || !aligned(g->dh0, 4))
+        return GEM_EALIGN;
+    a.states = states;
+    if (!ssm_fits(*s, true, ops->dev)) return GEM_ESCRATCH;
+    OPS_HIP(gemk::launch_ssm_backward(a, s->dtype == GEM_BF16, ops->dev, ops->stream));
     return GEM_OK;
 }
 

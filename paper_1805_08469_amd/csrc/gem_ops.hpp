@@ -85,6 +85,20 @@ struct ConvBackArgs {
     void* dbefore;
 };
 
+struct SsmArgs {
+    gem_ssm s;             // strides filled in
+    void* y;
+    int64_t y_stride;
+    float* h_last;
+    float* states;
+};
+
+struct SsmBackArgs {
+    gem_ssm s;
+    const float* states;
+    gem_ssm_grad g;        // strides filled in
+};
+
 struct ScanArgs {
     gem_scan s;            // strides filled in
     void* y;
@@ -124,6 +138,11 @@ int64_t conv_rows(int64_t tokens, int64_t channels);
 int64_t conv_scratch_bytes(int64_t tokens, int64_t channels);
 hipError_t launch_conv_forward(const ConvArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_conv_backward(const ConvBackArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
+int64_t ssm_rows(int64_t tokens, int64_t sequences, bool offsets, int64_t channels);
+int64_t ssm_bytes(int64_t tokens, int64_t sequences, bool offsets, int64_t channels, int64_t state, bool back);
+int64_t ssm_scratch_bytes(int64_t tokens, int64_t channels, int64_t state);
+hipError_t launch_ssm_forward(const SsmArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
+hipError_t launch_ssm_backward(const SsmBackArgs& a, bool bf16, const OpsDevice& d, hipStream_t stream);
 int64_t scan_rows(int64_t tokens, int64_t channels);
 int64_t scan_bytes(int64_t tokens, int64_t channels);            // of a launch
 int64_t scan_scratch_bytes(int64_t tokens, int64_t channels);    // of it and of any smaller one

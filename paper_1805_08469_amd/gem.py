@@ -43,6 +43,7 @@ GEM_VOCAB_MAX = 1 << 22
 GEM_TOP_MAX = 128
 GEM_TOKENS_MAX = (1 << 31) - 256
 GEM_CONV_MAX = 4
+GEM_STATE_MAX = 16
 
 # Every symbol include/gem.h declares.
 EXPORTED = (
@@ -56,7 +57,8 @@ EXPORTED = (
     "gem_ops_create", "gem_ops_destroy", "gem_token_scores", "gem_distill_loss",
     "gem_distill_grad", "gem_policy_loss", "gem_policy_grad", "gem_embed_forward",
     "gem_embed_scratch", "gem_embed_backward", "gem_conv_forward", "gem_conv_scratch",
-    "gem_conv_backward", "gem_scan_scratch", "gem_scan_state_rows",
+    "gem_conv_backward", "gem_ssm_scratch", "gem_ssm_state_rows", "gem_ssm_forward",
+    "gem_ssm_backward", "gem_scan_scratch", "gem_scan_state_rows",
     "gem_scan_forward", "gem_scan_backward",
 )
 
@@ -125,6 +127,21 @@ class gem_conv(C.Structure):
                 ("x_stride", C.c_int64), ("channels", C.c_int32), ("sequences", C.c_int32),
                 ("width", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32),
                 ("reserved", C.c_int32)]
+
+
+class gem_ssm(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "dt", "b", "c", "z", "a", "d", "dt_bias", "h0",
+                                          "offsets")] + \
+               [(n, C.c_int64) for n in ("tokens", "x_stride", "dt_stride", "b_stride", "c_stride",
+                                         "z_stride")] + \
+               [(n, C.c_int32) for n in ("channels", "state", "sequences", "dtype")]
+
+
+class gem_ssm_grad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dy", "dh_last", "dx", "ddt", "db", "dc", "dz", "da",
+                                          "dd", "ddt_bias", "dh0")] + \
+               [(n, C.c_int64) for n in ("dy_stride", "dx_stride", "ddt_stride", "db_stride",
+                                         "dc_stride", "dz_stride")]
 
 
 class gem_scan(C.Structure):
@@ -211,6 +228,10 @@ def _load():
         "gem_conv_scratch": (C.c_int, [C.c_int64, C.c_int32, i64p]),
         "gem_conv_backward": (C.c_int, [vp, C.POINTER(gem_conv), vp, C.c_int64, vp, vp, C.c_int64,
                                         vp, vp, vp]),
+        "gem_ssm_scratch": (C.c_int, [C.c_int64, C.c_int32, C.c_int32, i64p]),
+        "gem_ssm_state_rows": (C.c_int, [C.c_int64, i64p]),
+        "gem_ssm_forward": (C.c_int, [vp, C.POINTER(gem_ssm), vp, C.c_int64, vp, vp]),
+        "gem_ssm_backward": (C.c_int, [vp, C.POINTER(gem_ssm), vp, C.POINTER(gem_ssm_grad)]),
         "gem_scan_scratch": (C.c_int, [C.c_int64, C.c_int32, i64p]),
         "gem_scan_state_rows": (C.c_int, [C.c_int64, i64p]),
         "gem_scan_forward": (C.c_int, [vp, C.POINTER(gem_scan), vp, C.c_int64, vp, vp]),
@@ -538,6 +559,26 @@ def gem_conv_backward(ops: int, s: gem_conv, dy: int, dy_stride: int, dlast: int
                                 dbias, dbefore), "gem_conv_backward")
 
 
+def gem_ssm_scratch(tokens: int, channels: int, state: int) -> int:
+    out = C.c_int64()
+    _check(_L.gem_ssm_scratch(tokens, channels, state, C.byref(out)), "gem_ssm_scratch")
+    return out.value
+
+
+def gem_ssm_state_rows(tokens: int) -> int:
+    out = C.c_int64()
+    _check(_L.gem_ssm_state_rows(tokens, C.byref(out)), "gem_ssm_state_rows")
+    return out.value
+
+
+def gem_ssm_forward(ops: int, s: gem_ssm, y: int, y_stride: int, h_last: int, states: int) -> None:
+    _check(_L.gem_ssm_forward(ops, C.byref(s), y, y_stride, h_last, states), "gem_ssm_forward")
+
+
+def gem_ssm_backward(ops: int, s: gem_ssm, states: int, g: gem_ssm_grad) -> None:
+    _check(_L.gem_ssm_backward(ops, C.byref(s), states, C.byref(g)), "gem_ssm_backward")
+
+
 def gem_scan_scratch(tokens: int, channels: int) -> int:
     out = C.c_int64()
     _check(_L.gem_scan_scratch(tokens, channels, C.byref(out)), "gem_scan_scratch")
@@ -712,6 +753,25 @@ class Ops:
         s = gem_conv(x, weight, bias, before, offsets, tokens, x_stride, channels, sequences, width,
                      dtype, act, 0)
         gem_conv_backward(self.h, s, dy, dy_stride, dlast, dx, dx_stride, dweight, dbias, dbefore)
+
+    def ssm_forward(self, x, dt, b, c, a, tokens, channels, state, sequences, dtype, y, z=None,
+                    d=None, dt_bias=None, h0=None, offsets=None, h_last=None, states=None,
+                    x_stride=0, dt_stride=0, b_stride=0, c_stride=0, z_stride=0, y_stride=0):
+        s = gem_ssm(x, dt, b, c, z, a, d, dt_bias, h0, offsets, tokens, x_stride, dt_stride,
+                    b_stride, c_stride, z_stride, channels, state, sequences, dtype)
+        gem_ssm_forward(self.h, s, y, y_stride, h_last, states)
+
+    def ssm_backward(self, x, dt, b, c, a, tokens, channels, state, sequences, dtype, states, dy,
+                     dx, ddt, db, dc, z=None, d=None, dt_bias=None, h0=None, offsets=None,
+                     dh_last=None, dz=None, da=None, dd=None, ddt_bias=None, dh0=None, x_stride=0,
+                     dt_stride=0, b_stride=0, c_stride=0, z_stride=0, dy_stride=0, dx_stride=0,
+                     ddt_stride=0, db_stride=0, dc_stride=0, dz_stride=0):
+        s = gem_ssm(x, dt, b, c, z, a, d, dt_bias, h0, offsets, tokens, x_stride, dt_stride,
+                    b_stride, c_stride, z_stride, channels, state, sequences, dtype)
+        gem_ssm_backward(self.h, s, states,
+                         gem_ssm_grad(dy, dh_last, dx, ddt, db, dc, dz, da, dd, ddt_bias, dh0,
+                                      dy_stride, dx_stride, ddt_stride, db_stride, dc_stride,
+                                      dz_stride))
 
     def scan_forward(self, x, gate, tokens, channels, sequences, dtype, y, offsets=None, h0=None,
                      h_last=None, states=None, x_stride=0, gate_stride=0, y_stride=0):

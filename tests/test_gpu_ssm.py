@@ -1,0 +1,422 @@
+"""The selective scan and its backward pass against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import ssm_reference
+from paper_1805_08469_amd import gem as G
+
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+KIND = {torch.float32: G.GEM_F32, torch.bfloat16: G.GEM_BF16}
+F32, BF16 = torch.float32, torch.bfloat16
+OUT = ("y", "h_last", "dx", "ddt", "db", "dc", "dz", "da", "dd", "ddt_bias", "dh0")
+
+
+def cuts(kind, tokens, seqs, g):
+    if kind == "equal":
+        return [tokens // seqs * i for i in range(seqs + 1)]
+    c = sorted(int(v) for v in torch.randint(tokens + 1, (seqs - 1,), generator=g))
+    if seqs > 4:
+        c[1] = c[0]                       # empty, and one of a token
+        c[3] = min(c[2] + 1, tokens)
+        c.sort()
+    return [0] + c + [tokens]
+
+
+def wide(rows, cols, pad, dtype, g=None, scale=1.0):
+    t = torch.full((rows, cols + pad), 7.0, device="cuda", dtype=dtype)
+    if g is not None:
+        t[:, :cols] = (torch.randn(rows, cols, generator=g) * scale).cuda()
+    return t[:, :cols]
+
+
+def make(tokens, seqs, D, N, dtype, pad=0, kind="equal", gated=True, seed=0):
+    g = torch.Generator().manual_seed(seed + 31 * tokens + D)
+    s = {n: wide(tokens, D, pad, dtype, g) for n in ("x", "dt", "dy")}
+    s.update({n: wide(tokens, N, pad, dtype, g) for n in ("b", "c")})
+    s["z"] = wide(tokens, D, pad, dtype, g) if gated else None
+    s["a"] = -(torch.arange(1, N + 1) * torch.exp(torch.randn(D, N, generator=g) * 0.3)).cuda()
+    s["d"], s["dt_bias"] = torch.randn(D, generator=g).cuda(), (torch.randn(D, generator=g) * 2 - 3).cuda()
+    s["h0"], s["dh_last"] = torch.randn(seqs, D, N, generator=g).cuda(), torch.randn(seqs, D, N, generator=g).cuda()
+    s["off"] = cuts(kind, tokens, seqs, g)
+    s["offsets"] = torch.tensor(s["off"], device="cuda") if kind != "equal" else None
+    return s
+
+
+def outputs(s):
+    tokens, D, N, dtype = *s["x"].shape, s["b"].shape[1], s["x"].dtype
+    pad = s["x"].stride(0) - D if tokens else 0
+    r = {n: wide(tokens, D, pad, dtype) for n in ("y", "dx", "ddt", "dz")}
+    r.update({n: wide(tokens, N, pad, dtype) for n in ("db", "dc")})
+    r.update({n: torch.full_like(s[m], 7) for n, m in dict(h_last="h0", da="a", dd="d", ddt_bias="dt_bias", dh0="h0").items()})
+    r["states"] = torch.full((G.gem_ssm_state_rows(tokens), D, N), 7.0, device="cuda")
+    if s["z"] is None:
+        del r["dz"]
+    return r
+
+
+def ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def arguments(s):
+    tokens, D, N = *s["x"].shape, s["b"].shape[1]
+    strides = {n + "_stride": s[n].stride(0) if s[n] is not None and tokens else 0 for n in ("x", "dt", "b", "c", "z")}
+    return ([s[n].data_ptr() for n in ("x", "dt", "b", "c", "a")] + [tokens, D, N, len(s["off"]) - 1, KIND[s["x"].dtype]],
+            dict(z=ptr(s["z"]), d=ptr(s["d"]), dt_bias=ptr(s["dt_bias"]), h0=ptr(s["h0"]), offsets=ptr(s["offsets"]), **strides))
+
+
+def forward(ops, s, r, **k):
+    args, named = arguments(s)
+    ops.ssm_forward(*args, y=r["y"].data_ptr(), y_stride=r["y"].stride(0) if s["x"].shape[0] else 0,
+                    **{**dict(h_last=ptr(r.get("h_last")), states=ptr(r.get("states"))), **named, **k})
+
+
+def backward(ops, s, r, **k):
+    args, named = arguments(s)
+    rows = [n for n in ("dx", "ddt", "db", "dc", "dz") if n in r]
+    if s["x"].shape[0]:
+        named.update({n + "_stride": r[n].stride(0) for n in rows}, dy_stride=s["dy"].stride(0))
+    ops.ssm_backward(*args, states=r["states"].data_ptr(), dy=s["dy"].data_ptr(), dh_last=ptr(s["dh_last"]),
+                     **{n: ptr(r.get(n)) for n in OUT[2:]}, **{**named, **k})
+
+
+def ops_for(s, stream=None):
+    tokens, D, N = *s["x"].shape, s["b"].shape[1]
+    return G.Ops(G.gem_ssm_scratch(tokens, D, N), stream or torch.cuda.current_stream().cuda_stream)
+
+
+def check(r, want, names=OUT):
+    for n in names:
+        if n not in want or n not in r:
+            continue
+        v, e = want[n]
+        got = r[n].double().cpu().numpy()
+        off = np.abs(got - v) - e - np.abs(v) * HALF[r[n].dtype]
+        assert not np.isnan(got).any() and (off <= 0).all(), (n, float(np.nanmax(off)), np.unravel_index(np.nanargmax(off), off.shape))
+
+
+def wanted(s, backward=True):
+    return ssm_reference.scan({k: v.double().cpu().numpy() if v is not None else None for k, v in s.items()
+                               if k not in ("off", "offsets")}, s["off"], backward)
+
+
+CASES = [(1, 1, 1, 1, "equal"), (1, 1, 64, 16, "equal"), (6, 6, 65, 16, "equal"), (7, 1, 3, 5, "equal"), (8, 2, 130, 16, "equal"),
+         (33, 3, 66, 9, "equal"), (40, 8, 17, 8, "equal"), (129, 1, 64, 16, "equal"), (300, 4, 70, 16, "equal"),
+         (300, 7, 64, 16, "ragged"), (301, 9, 37, 3, "ragged"), (520, 1, 5, 2, "equal"), (700, 12, 130, 16, "ragged"),
+         (2600, 2, 64, 16, "equal")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tokens,seqs,D,N,kind", CASES)
+def test_forward_and_backward(tokens, seqs, D, N, kind, dtype):
+    """Sequences taken whole and cut, packed with empty ones, states of all numbers, gated and not."""
+    for gated, pad in ((True, 0), (False, 3)):
+        s = make(tokens, seqs, D, N, dtype, pad, kind, gated)
+        r, again = outputs(s), outputs(s)
+        with ops_for(s) as ops:
+            forward(ops, s, r)
+            backward(ops, s, r)
+            check(r, wanted(s))
+            forward(ops, s, again)
+            backward(ops, s, again)
+            assert all(torch.equal(r[n], again[n]) for n in r if n != "states")
+            if pad:
+                for n in ("y", "dx", "ddt", "db", "dc"):
+                    t = r[n]
+                    whole = t.as_strided((tokens, t.shape[1] + pad), (t.stride(0), 1))
+                    assert (whole[:, t.shape[1]:] == 7).all(), n
+            h = s["h0"].clone()            # kept in place
+            forward(ops, dict(s, h0=h), dict(again, h_last=h))
+            assert torch.equal(h, r["h_last"]) and torch.equal(again["y"], r["y"])
+
+
+@pytest.mark.gpu
+def test_longer_runs():
+    """Enough channels for runs of 24 tokens; float states through three of them."""
+    s = make(700, 5, 4096, 16, BF16, 0, "ragged")
+    r = outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, r)
+        backward(ops, s, r)
+    check(r, wanted(s))
+
+
+@pytest.mark.gpu
+def test_longest_runs():
+    """Runs of 256 tokens: two sequences, and the same tokens as four with their states handed on, which
+    are cut at other places.  Decays of 0.2 a token and less forget a run's start to below a rounding,
+    so outputs agree to the roundings of some ten steps (of a step: 8 of the state, N + 4 of the sum)."""
+    T, D, N = 16384, 2112, 16
+    s = make(T, 2, D, N, F32, gated=False)
+    s["dt_bias"] += 5
+    r = outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, r)
+        h, y = s["h0"].clone(), torch.empty_like(r["y"])
+        for part in range(2):
+            at = torch.cat([torch.arange(q * T // 2 + part * T // 4, q * T // 2 + (part + 1) * T // 4) for q in range(2)]).cuda()
+            p = dict(s, h0=h, off=[0, T // 4, T // 2], **{n: s[n][at].contiguous() for n in ("x", "dt", "b", "c")})
+            q = dict(y=torch.empty(T // 2, D, device="cuda"), h_last=h)
+            forward(ops, p, q)
+            y[at] = q["y"]
+    size = (s["c"].abs().sum(1, keepdim=True) * 40 + s["x"].abs() * s["d"].abs()).clamp(min=1.0)
+    assert ((y - r["y"]).abs() <= 2.0 ** -24 * 120 * size).all()
+    assert ((h - r["h_last"]).abs() <= 2.0 ** -24 * 120 * (1 + h.abs())).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,N", [(1, 16), (130, 16), (257, 7)])
+def test_tokens_one_at_a_time_are_a_sequence(D, N, dtype):
+    """Answers from states kept in place, without scratch: the bits of the whole sequences' call, as far
+    as that is not cut."""
+    seqs, n = 5, 9
+    s = make(seqs * n, seqs, D, N, dtype)
+    r = outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, r)
+    y = r["y"].contiguous().view(seqs, n, D)
+    h = s["h0"].clone()
+    with G.Ops(0, torch.cuda.current_stream().cuda_stream) as ops:
+        for t in range(n):
+            one = {k: s[k].contiguous().view(seqs, n, -1)[:, t].contiguous() for k in ("x", "dt", "b", "c", "z")}
+            out = dict(y=torch.empty(seqs, D, device="cuda", dtype=dtype), h_last=h)
+            forward(ops, dict(s, h0=h, off=list(range(seqs + 1)), **one), out)
+            assert torch.equal(out["y"], y[:, t])
+    assert torch.equal(h, r["h_last"])
+
+
+def test_gradients_are_those_of_differences():
+    """Central differences of the 64-bit forward pass in every input, against its formulas: the kernel is
+    held to those above."""
+    off, rng = [0, 4, 4, 9], np.random.default_rng(0)
+    T, D, N = 9, 3, 4
+    s = {n: rng.standard_normal((T, D)) for n in ("x", "dt", "z", "dy")}
+    s.update({n: rng.standard_normal((T, N)) for n in ("b", "c")}, d=rng.standard_normal(D), dt_bias=rng.standard_normal(D))
+    s.update({n: rng.standard_normal((3, D, N)) for n in ("h0", "dh_last")}, a=-np.exp(rng.standard_normal((D, N))))
+
+    def loss(v):
+        r = ssm_reference.scan(v, off, False)
+        return (r["y"][0] * s["dy"]).sum() + (r["h_last"][0] * s["dh_last"]).sum()
+
+    want = ssm_reference.scan(s, off)
+    for name, grad in dict(x="dx", dt="ddt", b="db", c="dc", z="dz", a="da", d="dd", dt_bias="ddt_bias", h0="dh0").items():
+        direction = rng.standard_normal(s[name].shape)
+        up, down = dict(s, **{name: s[name] + 1e-5 * direction}), dict(s, **{name: s[name] - 1e-5 * direction})
+        slope = (loss(up) - loss(down)) / 2e-5
+        assert abs(slope - (want[grad][0] * direction).sum()) < 1e-6 * (1 + abs(slope)), name
+
+
+@pytest.mark.gpu
+def test_left_out():
+    """No skip, bias, first states or gate; no tokens; what is not asked for."""
+    s = make(90, 4, 70, 16, F32, 0, "ragged", gated=False)
+    zero = dict(s, **{n: torch.zeros_like(s[n]) for n in ("d", "dt_bias", "h0", "dh_last")})
+    r = outputs(s)
+    with ops_for(s) as ops:
+        bare = dict(s, d=None, dt_bias=None, h0=None, dh_last=None)
+        forward(ops, bare, r)
+        few = {n: t for n, t in r.items() if n not in ("da", "dd", "ddt_bias", "dh0")}
+        backward(ops, bare, few)
+        check(r, wanted(zero), ("y", "h_last", "dx", "ddt", "db", "dc"))
+        assert all((r[n] == 7).all() for n in ("da", "dd", "ddt_bias", "dh0"))
+        e = make(0, 3, 70, 16, F32)
+        r = outputs(e)
+        forward(ops, e, r)
+        backward(ops, e, r)
+        assert torch.equal(r["h_last"], e["h0"]) and torch.equal(r["dh0"], e["dh_last"])
+        assert all((r[n] == 0).all() for n in ("da", "dd", "ddt_bias"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N", [16, 6])
+def test_values_at_the_ends(N):
+    """Steps from nothing to large ones: softplus of -60 to 60, and states that a step forgets."""
+    s = make(60, 2, 67, N, F32)
+    s["dt"][:] = torch.linspace(-60, 60, 60, device="cuda")[:, None]
+    s["dt_bias"][:] = 0
+    r = outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, r)
+        backward(ops, s, r)
+    check(r, wanted(s))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,tokens", [("ragged", 400), ("equal", 400)])
+def test_nothing_passes_between_sequences(kind, tokens):
+    """No numbers in one sequence and its state leave the others as they are."""
+    s = make(tokens, 8, 70, 16, F32, 0, kind, seed=3)
+    r, first = outputs(s), outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, first)
+        backward(ops, s, first)
+        q = max(range(8), key=lambda k: s["off"][k + 1] - s["off"][k])
+        a, b = s["off"][q], s["off"][q + 1]
+        for n in ("x", "dt", "b", "c", "z", "dy"):
+            s[n][a:b] = float("nan")
+        s["h0"][q], s["dh_last"][q] = float("inf"), float("-inf")
+        forward(ops, s, r)
+        backward(ops, s, r)
+    rest, others = [t for t in range(tokens) if not a <= t < b], [k for k in range(8) if k != q]
+    for n in ("y", "dx", "ddt", "db", "dc", "dz"):
+        assert torch.equal(r[n][rest], first[n][rest]) and r[n][a:b].isnan().all(), n
+    for n in ("h_last", "dh0"):
+        assert torch.equal(r[n][others], first[n][others]), n
+
+
+@pytest.mark.gpu
+def test_offsets_of_any_values_stay_in_the_arrays():
+    """They are not checked on the host; every array stands between values that are watched."""
+    n, seqs = 60, 5
+    for bad in ([0, 70, 10, -5, 900, 60], [5, 4, 3, 2, 1, 0], [0] * 6, [60] * 6, [-2 ** 62, 2 ** 62, 3, 3, 40, 2 ** 40], [10, 20, 30, 40, 50, 55]):
+        s = make(n, seqs, 33, 16, F32, 0, "ragged")
+        s["offsets"] = torch.tensor(bad, device="cuda")
+        r = outputs(s)
+        room = {k: torch.full((3 * t.numel(),), 7.0, device="cuda") for k, t in r.items()}
+        r = {k: room[k][t.numel():2 * t.numel()].view(t.shape) for k, t in r.items()}
+        with ops_for(s) as ops:
+            forward(ops, s, r)
+            backward(ops, s, r)
+            torch.cuda.synchronize()
+            for k, t in r.items():
+                assert (room[k][:t.numel()] == 7).all() and (room[k][2 * t.numel():] == 7).all(), (bad, k)
+            h = s["h0"].clone()
+            forward(ops, dict(s, h0=h), dict(r, h_last=h))
+            torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_same_bits_on_a_stream_and_in_graphs():
+    stream = torch.cuda.Stream()
+    sets = [make(1200 + 16 * i, 4, 130, 16, BF16, 0, "equal", seed=i) for i in range(2)]
+    outs = [outputs(s) for s in sets]
+    torch.cuda.synchronize()
+    with ops_for(sets[1], stream.cuda_stream) as ops:
+        want, graphs = [], []
+        for s, r in zip(sets, outs):
+            forward(ops, s, r)
+            backward(ops, s, r)
+            stream.synchronize()
+            want.append({n: t.clone() for n, t in r.items()})
+        for s, r in zip(sets, outs):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                forward(ops, s, r)
+                backward(ops, s, r)
+            graphs.append(graph)
+        for _ in range(3):
+            for s, r, graph, w in zip(sets, outs, graphs, want):
+                for t in r.values():
+                    t.fill_(5)
+                torch.cuda.synchronize()
+                with torch.cuda.stream(stream):
+                    graph.replay()
+                stream.synchronize()
+                assert all(torch.equal(r[n], w[n]) for n in w)
+        del graphs
+
+
+@pytest.mark.gpu
+def test_more_elements_than_32_bits_count():
+    """The last tokens of an array of more, in a sequence of their own."""
+    T, D, N = 1048576 + 40, 2112, 1
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, dt = torch.zeros(T, D, device="cuda", dtype=BF16), torch.zeros(T, D, device="cuda", dtype=BF16)
+    x[-40:], dt[-40:] = (torch.randn(40, D, device="cuda", generator=g).to(BF16) for _ in range(2))
+    b, c = (torch.randn(T, N, device="cuda", generator=g).to(BF16) for _ in range(2))
+    a = -torch.ones(D, N, device="cuda")
+    off = torch.tensor([0, T - 40, T], device="cuda")
+    y, small = torch.empty_like(x), torch.empty(40, D, device="cuda", dtype=BF16)
+    h, h_small = torch.empty(2, D, N, device="cuda"), torch.empty(1, D, N, device="cuda")
+    with G.Ops(G.gem_ssm_scratch(T, D, N) if G.gem_ssm_scratch(T, D, N) < 2 ** 35 else 2 ** 35, torch.cuda.current_stream().cuda_stream) as ops:
+        ops.ssm_forward(x.data_ptr(), dt.data_ptr(), b.data_ptr(), c.data_ptr(), a.data_ptr(), T, D, N, 2, 1, y=y.data_ptr(),
+                        offsets=off.data_ptr(), h_last=h.data_ptr())
+        tail = [t[-40:].contiguous() for t in (x, dt, b, c)]
+        ops.ssm_forward(*[t.data_ptr() for t in tail], a.data_ptr(), 40, D, N, 1, 1, y=small.data_ptr(), h_last=h_small.data_ptr())
+    # Cut at other places: two roundings of bfloat16 apart at most.
+    assert ((y[-40:].float() - small.float()).abs() <= 2.0 ** -7 * small.float().abs() + 1e-5).all()
+    assert ((h[1] - h_small[0]).abs() <= 2.0 ** -24 * 100 * (1 + h_small[0].abs())).all()
+    assert (y[:T - 40] == 0).all()
+
+
+def cut(tokens, sequences, offsets, channels):
+    """Runs of a call: their number, and whether they begin with sequences."""
+    slices = -(-channels // 64)
+    length = tokens * slices // 2048
+    if not offsets:
+        one, most = tokens // sequences, min(length, 256)
+        if one <= 16 or one <= most or (one <= 4096 and sequences * slices >= 1024):
+            return -(-tokens // (one * max(1, most // one))), True
+    length = min(256, max(16, -(-length // 8) * 8))
+    return -(-tokens // length), False
+
+
+@pytest.mark.parametrize("channels", [1, 64, 65, 130, 1001, 2048, 4100, 8192, 70000])
+def test_scratch_holds_every_shorter_batch(channels):
+    """Floats of the runs' states, steps and what reaches them, of the slices' gradients of b and c, and of
+    the runs' of the parameters."""
+    N = 16
+    slices = -(-channels // 64)
+    worst = before = 0
+    for tokens in sorted(set(list(range(1, 70000, 61)) + [2 ** k + d for k in range(4, 22) for d in (-1, 0, 1)])):
+        now = G.gem_ssm_scratch(tokens, channels, N)
+        for sequences in {1, 2, 24, max(1, tokens // 16), max(1, tokens // 17), max(1, tokens // 100), max(1, tokens // 4097), tokens}:
+            for offsets in (True, False):
+                if not offsets and tokens % sequences:
+                    continue
+                count, _ = cut(tokens, sequences, offsets, channels)
+                taken = 4 * (count * channels * (2 * N + 1 + N + 2) + slices * tokens * 32)
+                worst = max(worst, taken)
+        assert now >= worst and now >= before, tokens
+        assert G.gem_ssm_scratch(tokens, channels + 1, N) >= now and G.gem_ssm_scratch(tokens, channels, N - 1) <= now
+        before = now
+
+
+def test_refusals():
+    """On the host, before any work is queued."""
+    L, C, n = G.lib(), G.C, G.C.c_int64()
+    fake = 1 << 20
+
+    def ssm(**k):
+        s = G.gem_ssm(x=64, dt=64, b=64, c=64, z=64, a=64, tokens=4, channels=8, state=4, sequences=2)
+        for name, v in k.items():
+            setattr(s, name, v)
+        return s
+
+    def forward(y=64, stride=0, h_last=None, states=None, ops=fake, **k):
+        s = ssm(**k)
+        return L.gem_ssm_forward(ops, C.byref(s), y, stride, h_last, states)
+
+    def backward(grad=None, states=64, ops=fake, **k):
+        s, g = ssm(**k), G.gem_ssm_grad(dy=64, dx=64, ddt=64, db=64, dc=64, dz=64)
+        for name, v in (grad or {}).items():
+            setattr(g, name, v)
+        return L.gem_ssm_backward(ops, C.byref(s), states, C.byref(g))
+
+    assert L.gem_ssm_forward(fake, None, 64, 0, None, None) == G.GEM_EINVAL
+    s = ssm()
+    assert L.gem_ssm_backward(fake, C.byref(s), 64, None) == G.GEM_EINVAL
+    for f in (forward, backward):
+        for k in [dict(ops=None)] + [{m: None} for m in ("x", "dt", "b", "c", "a")] + \
+                [{m: 7} for m in ("x_stride", "dt_stride", "z_stride")] + [{m: 3} for m in ("b_stride", "c_stride")] + \
+                [dict(tokens=-2), dict(tokens=3), dict(channels=0), dict(sequences=0), dict(state=0), dict(state=17),
+                 dict(tokens=G.GEM_TOKENS_MAX + 1, sequences=1), dict(channels=2 ** 26), dict(tokens=2 ** 30, channels=2 ** 24, state=1, sequences=1)]:
+            assert f(**k) == G.GEM_EINVAL, k
+        assert f(dtype=7) == G.GEM_EDTYPE
+        for m in ("x", "dt", "b", "c", "z", "a", "d", "dt_bias", "h0", "offsets"):
+            assert f(**{m: 66}) == G.GEM_EALIGN, m
+    assert forward(y=None) == forward(stride=7) == G.GEM_EINVAL
+    assert forward(y=66) == forward(h_last=66) == forward(states=66) == G.GEM_EALIGN
+    for m in ("dy", "dx", "ddt", "db", "dc"):
+        assert backward({m: None}) == G.GEM_EINVAL, m
+        assert backward({m + "_stride": 3}) == G.GEM_EINVAL, m
+    assert backward(states=None) == backward(z=None) == G.GEM_EINVAL
+    for m in ("dy", "dx", "ddt", "db", "dc", "dz", "dh_last", "da", "dd", "ddt_bias", "dh0"):
+        assert backward({m: 66}) == G.GEM_EALIGN, m
+    assert backward(states=66) == G.GEM_EALIGN
+    for bad in ((-1, 1, 1), (2 ** 31 - 1, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 17), (1, 2 ** 27, 2)):
+        assert L.gem_ssm_scratch(*bad, C.byref(n)) == G.GEM_EINVAL
+    assert L.gem_ssm_scratch(1, 1, 1, None) == L.gem_ssm_state_rows(-1, C.byref(n)) == G.GEM_EINVAL

@@ -15,9 +15,11 @@
 // A run's tokens are one map h -> exp(A sum u) h + h', so runs are joined as in the gated recurrence: the
 // maps of all runs, their composition, and the walk again from the state that reaches each run.  Runs
 // that begin with a sequence need no maps.  Backward is the same from the last token: e_t = a_t (C_t dy_t +
-// e_{t+1}), and forms eight states at a time again from the one that forward kept for them.
+// e_{t+1}), and forms four states at a time again from the one that forward kept for eight tokens.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "gem_ops.hpp"
 #include "gem_ops_device.hpp"
@@ -73,13 +75,24 @@ __device__ __forceinline__ float softplus(float v)
     return (v > 0.0f ? v : 0.0f) + p * E;
 }
 
+// Element i of an array whose address is the wave's: a base in scalar registers, 32 bits of offset.
+template <class T> __device__ __forceinline__ T* element(T* base, uint32_t i)
+{
+    return reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<std::remove_const_t<T>*>(base)) + i * static_cast<uint32_t>(sizeof(T)));
+}
+
 // ---- what a lane has --------------------------------------------------------------------
 
 // Its own channel `mine` (of which it computes what is one value a channel), and states [n, n + S) of the
 // four channels from `first` on.  FULL: there are 4 S states, so that a lane's are whole.
 template <int S, bool FULL> struct Lane {
-    int mine, at, first, n, D, N;
+    int mine, first, D, N;
+    uint32_t at, n;
     bool in;
+
+    // Where the lane stands, as something new: else the addresses of a loop's loads are all formed ahead of
+    // it, 64 bits each, and spill.
+    __device__ __forceinline__ void here() { asm volatile("" : "+v"(at), "+v"(n)); }
 
     __device__ Lane(const gem_ssm& s, int slice)
     {
@@ -98,7 +111,7 @@ template <int S, bool FULL> struct Lane {
 #pragma unroll
         for (int j = 0; j < kQuad; ++j) {
             const bool there = first + j < D;
-            const float* row = block + static_cast<int64_t>(there ? first + j : D - 1) * N;
+            const float* row = element(block, static_cast<uint32_t>(there ? first + j : D - 1) * N);
             if constexpr (FULL) {
                 using V = float __attribute__((ext_vector_type(S), aligned(4)));
                 const V v = *reinterpret_cast<const V*>(row + n);
@@ -107,8 +120,9 @@ template <int S, bool FULL> struct Lane {
             } else {
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    const float v = row[n + s < N ? n + s : N - 1];
-                    h[j][s] = there && n + s < N ? v : 0.0f;
+                    const bool has = static_cast<int>(n) + s < N;
+                    const float v = *element(row, has ? n + s : N - 1);
+                    h[j][s] = there && has ? v : 0.0f;
                 }
             }
         }
@@ -118,7 +132,7 @@ template <int S, bool FULL> struct Lane {
 #pragma unroll
         for (int j = 0; j < kQuad; ++j) {
             if (first + j >= D) continue;
-            float* row = block + static_cast<int64_t>(first + j) * N;
+            float* row = element(block, static_cast<uint32_t>(first + j) * N);
             if constexpr (FULL) {
                 using V = float __attribute__((ext_vector_type(S), aligned(4)));
                 V v;
@@ -128,7 +142,7 @@ template <int S, bool FULL> struct Lane {
             } else {
 #pragma unroll
                 for (int s = 0; s < S; ++s)
-                    if (n + s < N) row[n + s] = h[j][s];
+                    if (static_cast<int>(n) + s < N) row[n + s] = h[j][s];
             }
         }
     }
@@ -147,25 +161,30 @@ template <int S, bool FULL> struct Lane {
     template <class T> __device__ __forceinline__ void shared(const T* row, float (&v)[S]) const
     {
         if constexpr (FULL && sizeof(T) == 2 && S == 4) {
-            const Raw<T> r = *reinterpret_cast<const Raw<T>*>(row + n);
+            const Raw<T> r = *reinterpret_cast<const Raw<T>*>(element(row, n));
             widen(r[0], r[1], v);
         } else if constexpr (FULL && sizeof(T) == 4) {
             using V = float __attribute__((ext_vector_type(S), aligned(4)));
-            const V r = *reinterpret_cast<const V*>(row + n);
+            const V r = *reinterpret_cast<const V*>(element(row, n));
 #pragma unroll
             for (int s = 0; s < S; ++s) v[s] = r[s];
         } else {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                const float r = load(row, n + s < N ? n + s : N - 1);
-                v[s] = n + s < N ? r : 0.0f;
+                const bool has = static_cast<int>(n) + s < N;
+                const float r = load(element(row, has ? n + s : N - 1), 0);
+                v[s] = has ? r : 0.0f;
             }
         }
     }
+    // Its channel's value; where it has none, the last channel's.
     template <class T> __device__ __forceinline__ float own(const void* array, int64_t stride, int t) const
     {
-        const float v = load(static_cast<const T*>(array) + t * stride, at);
-        return in ? v : 0.0f;
+        return load(element(static_cast<const T*>(array) + t * stride, at), 0);
+    }
+    template <class T> __device__ __forceinline__ void write(void* array, int64_t stride, int t, float v) const
+    {
+        if (in) store(element(static_cast<T*>(array) + t * stride, at), 0, v);
     }
     __device__ __forceinline__ float weight(const float* w) const { return w && in ? w[at] : 0.0f; }
 };
@@ -191,21 +210,25 @@ __device__ __forceinline__ bool row_of(const Runs& r, int tokens, Row& out)
     const uint32_t run = i / static_cast<uint32_t>(r.slices);
     if (run >= static_cast<uint32_t>(r.count)) return false;
     out.run = static_cast<int>(run);
-    out.slice = static_cast<int>(i - run * r.slices);
+    // Blocks go to the eight dies in turn: turned by a block a run, slices visit all of them, and each
+    // die's cache has all of its channels at work where rows are a power of two long.
+    out.slice = static_cast<int>((i + kWaves * run) % static_cast<uint32_t>(r.slices));
     out.t0 = out.run * r.len;
     out.t1 = tokens - out.t0 > r.len ? out.t0 + r.len : tokens;
     return true;
 }
 
-// kStep tokens from one at which a state is kept: bits of those that are the run's, that begin a sequence,
-// and that end one.  begin and end are a sequence's that some token of the window before belongs to (the
+// kSpan tokens: bits of those that are the run's, that begin a sequence, and that end one.  begin and end are a sequence's that some token of the window before belongs to (the
 // last one scanned): where it reaches over all of this one, nothing begins or ends here.
+constexpr int kSpan = 4;                   // tokens whose inputs a lane has at a time
+static_assert(kStateTokens == 2 * kSpan, "every other span begins where a state is kept");
+
 struct Window {
     uint32_t valid, starts, ends;
 };
 __device__ __forceinline__ Window window_of(const Bounds& bound, int w, const Row& row, int& begin, int& end)
 {
-    const int u0 = w > row.t0 ? w : row.t0, u1 = w + kStep < row.t1 ? w + kStep : row.t1;
+    const int u0 = w > row.t0 ? w : row.t0, u1 = w + kSpan < row.t1 ? w + kSpan : row.t1;
     Window v{((1u << (u1 - w)) - 1) & ~((1u << (u0 - w)) - 1), 0, 0};
     if (begin < u0 && end > u1) return v;      // inside a sequence
     int q = bound.at(u0);
@@ -223,15 +246,23 @@ __device__ __forceinline__ Window window_of(const Bounds& bound, int w, const Ro
     return v;
 }
 
+// f(std::true_type) for a span that is all the run's and inside a sequence, which most are: there
+// nothing stands in a branch.
+template <class F> __device__ __forceinline__ void by_span(const Window& v, F f)
+{
+    if (v.valid == (1u << kSpan) - 1 && !(v.starts | v.ends)) f(std::true_type{});
+    else f(std::false_type{});
+}
+
 // ---- forward ---------------------------------------------------------------------------
 
 // OUT: the outputs, from the states that reach the runs; else the runs' maps.
 template <class T, int S, bool FULL, bool OUT>
-__global__ __launch_bounds__(kThreads) void forward_kernel(const SsmArgs a, const Runs runs, const Bounds bound)
+__global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const SsmArgs a, const Runs runs, const Bounds bound)
 {
     Row row;
     if (!row_of(runs, static_cast<int>(a.s.tokens), row)) return;
-    const Lane<S, FULL> o(a.s, row.slice);
+    Lane<S, FULL> o(a.s, row.slice);
     const int64_t DN = static_cast<int64_t>(o.D) * o.N;
     float A[kQuad][S], h[kQuad][S];
     o.get(a.s.a, A);
@@ -244,28 +275,31 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const SsmArgs a, cons
     float steps = 0.0f;
     bool cut = false;          // a sequence has begun in the run
     int begin = 0, end = -1;
-    for (int w = row.t0 / kStep * kStep; w < row.t1; w += kStep) {
+    for (int w = row.t0 / kSpan * kSpan; w < row.t1; w += kSpan) {
         const Window v = window_of(bound, w, row, begin, end);
-        float x[kStep], dt[kStep], z[kStep], B[kStep][S], C[kStep][S];
+        if (OUT && a.states && w % kStateTokens == 0 && (v.valid & 1)) o.put(a.states + static_cast<int64_t>(w / kStateTokens) * DN, h);
+        by_span(v, [&](auto inside) {
+        constexpr bool kInside = decltype(inside)::value;
+        o.here();
+        float x[kSpan], dt[kSpan], z[kSpan], B[kSpan][S], C[kSpan][S];
 #pragma unroll
-        for (int i = 0; i < kStep; ++i) {
-            if (!(v.valid >> i & 1)) continue;
+        for (int i = 0; i < kSpan; ++i) {
+            if (!kInside && !(v.valid >> i & 1)) continue;
             x[i] = o.template own<T>(a.s.x, a.s.x_stride, w + i);
             dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
             if (OUT && a.s.z) z[i] = o.template own<T>(a.s.z, a.s.z_stride, w + i);
             o.shared(static_cast<const T*>(a.s.b) + (w + i) * a.s.b_stride, B[i]);
             if (OUT) o.shared(static_cast<const T*>(a.s.c) + (w + i) * a.s.c_stride, C[i]);
         }
-        if (OUT && a.states && (v.valid & 1)) o.put(a.states + static_cast<int64_t>(w / kStateTokens) * DN, h);
 #pragma unroll
-        for (int i = 0; i < kStep; ++i) {
-            if (!(v.valid >> i & 1)) continue;
-            if (v.starts >> i & 1) {
+        for (int i = 0; i < kSpan; ++i) {
+            if (!kInside && !(v.valid >> i & 1)) continue;
+            if (!kInside && (v.starts >> i & 1)) {
                 o.get_or_zero(a.s.h0, bound.at(w + i), h);
                 steps = 0.0f;
                 cut = true;
             }
-            const float u = o.in ? softplus(dt[i] + bias) : 0.0f;
+            const float u = softplus(dt[i] + bias);
             float us[kQuad], ins[kQuad], ys[kQuad];
             spread(u, us);
             spread(u * x[i], ins);
@@ -286,13 +320,14 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(const SsmArgs a, cons
                 gates(z[i], g, r);
                 y *= z[i] * g;
             }
-            if (o.in) store(static_cast<T*>(a.y) + (w + i) * a.y_stride, o.mine, y);
-            if (a.h_last && (v.ends >> i & 1)) {
+            o.template write<T>(a.y, a.y_stride, w + i, y);
+            if (!kInside && a.h_last && (v.ends >> i & 1)) {
                 // Rows of the sequence's first tokens may still have to read h0.
                 if (runs.in_place && !cut) o.put(runs.reach + row.run * DN, h);
                 else o.put(a.h_last + bound.at(w + i) * DN, h);
             }
         }
+        });
     }
     if (!OUT) {
         o.put(runs.local + row.run * DN, h);
@@ -390,11 +425,11 @@ __global__ __launch_bounds__(kFoldThreads) void fold_kernel(const Runs r, const 
 // ---- backward ------------------------------------------------------------------------------
 
 template <class T, int S, bool FULL>
-__global__ __launch_bounds__(kThreads) void backward_map_kernel(const SsmBackArgs a, const Runs runs, const Bounds bound)
+__global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBackArgs a, const Runs runs, const Bounds bound)
 {
     Row row;
     if (!row_of(runs, static_cast<int>(a.s.tokens), row)) return;
-    const Lane<S, FULL> o(a.s, row.slice);
+    Lane<S, FULL> o(a.s, row.slice);
     float A[kQuad][S], e[kQuad][S];
     o.get(a.s.a, A);
 #pragma unroll
@@ -408,26 +443,29 @@ __global__ __launch_bounds__(kThreads) void backward_map_kernel(const SsmBackArg
     float steps = 0.0f;
     bool cut = false;
     int begin = 0, end = -1;
-    for (int w = (row.t1 - 1) / kStep * kStep; w + kStep > row.t0; w -= kStep) {
+    for (int w = (row.t1 - 1) / kSpan * kSpan; w + kSpan > row.t0; w -= kSpan) {
         const Window v = window_of(bound, w, row, begin, end);
-        float dt[kStep], z[kStep], dy[kStep], C[kStep][S];
+        by_span(v, [&](auto inside) {
+        constexpr bool kInside = decltype(inside)::value;
+        o.here();
+        float dt[kSpan], z[kSpan], dy[kSpan], C[kSpan][S];
 #pragma unroll
-        for (int i = 0; i < kStep; ++i) {
-            if (!(v.valid >> i & 1)) continue;
+        for (int i = 0; i < kSpan; ++i) {
+            if (!kInside && !(v.valid >> i & 1)) continue;
             dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
             if (a.s.z) z[i] = o.template own<T>(a.s.z, a.s.z_stride, w + i);
             dy[i] = o.template own<T>(a.g.dy, a.g.dy_stride, w + i);
             o.shared(static_cast<const T*>(a.s.c) + (w + i) * a.s.c_stride, C[i]);
         }
 #pragma unroll
-        for (int i = kStep - 1; i >= 0; --i) {
-            if (!(v.valid >> i & 1)) continue;
-            if (v.ends >> i & 1) {
+        for (int i = kSpan - 1; i >= 0; --i) {
+            if (!kInside && !(v.valid >> i & 1)) continue;
+            if (!kInside && (v.ends >> i & 1)) {
                 o.get_or_zero(a.g.dh_last, bound.at(w + i), e);
                 steps = 0.0f;
                 cut = true;
             }
-            const float u = o.in ? softplus(dt[i] + bias) : 0.0f;
+            const float u = softplus(dt[i] + bias);
             float d = dy[i];
             if (a.s.z) {
                 float g, r;
@@ -444,23 +482,28 @@ __global__ __launch_bounds__(kThreads) void backward_map_kernel(const SsmBackArg
                 for (int s = 0; s < S; ++s)
                     e[j][s] = __builtin_amdgcn_exp2f(us[j] * A[j][s]) * __builtin_fmaf(C[i][s], ds[j], e[j][s]);
         }
+        });
     }
     o.put(runs.local + static_cast<int64_t>(row.run) * o.D * o.N, e);
     if (o.in) runs.steps[static_cast<int64_t>(row.run) * o.D + o.mine] = cut ? -1.0f : steps;
 }
 
 template <class T, int S, bool FULL>
-__global__ __launch_bounds__(kThreads) void backward_kernel(const SsmBackArgs a, const Runs runs, const Bounds bound)
+__global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs a, const Runs runs, const Bounds bound)
 {
     constexpr int NP = kQuad * S;
     // The parts of dB and dC that each sixteen lanes (four channels' worth of fours) have.
-    __shared__ float parts[kWaves][kStep][4][2 * NP];
+    __shared__ float parts[kWaves][kSpan][4][2 * NP];
     Row row;
     if (!row_of(runs, static_cast<int>(a.s.tokens), row)) return;
-    const Lane<S, FULL> o(a.s, row.slice);
+    Lane<S, FULL> o(a.s, row.slice);
     const int64_t DN = static_cast<int64_t>(o.D) * o.N;
     const int lane = threadIdx.x % kWave;
-    float (&mine)[kStep][4][2 * NP] = parts[threadIdx.x / kWave];
+    float (&mine)[kSpan][4][2 * NP] = parts[threadIdx.x / kWave];
+    // A span's states, ahead of each token: with them in registers 200 of those spill.
+    using States = float __attribute__((ext_vector_type(S)));
+    __shared__ States kept[kWaves][kSpan][kQuad][kWave];
+    States (&ahead_of)[kSpan][kQuad][kWave] = kept[threadIdx.x / kWave];
     float A[kQuad][S], e[kQuad][S], dA[kQuad][S];
     o.get(a.s.a, A);
 #pragma unroll
@@ -474,20 +517,56 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const SsmBackArgs a,
     const float bias = o.weight(a.s.dt_bias), skip = o.weight(a.s.d);
     float dskip = 0.0f, dbias = 0.0f;
     int begin = 0, end = -1;
-    for (int w = (row.t1 - 1) / kStep * kStep; w + kStep > row.t0; w -= kStep) {
-        Window v = window_of(bound, w, row, begin, end);
-        // One sequence's tokens at a time, the last first: a state before a sequence's first token is not
-        // the one behind the token ahead of it.
-        for (uint32_t left = v.valid; left; left &= ~v.valid) {
-            const uint32_t begun = left & v.starts;
-            v.valid = begun ? left & (~0u << (31 - __builtin_clz(begun))) : left;
-            float x[kStep], dt[kStep], u[kStep], z[kStep], dy[kStep], B[kStep][S], C[kStep][S];
-            float h[kStep + 1][kQuad][S];          // before each token, and behind the last
-            if (v.valid & ~v.starts & 1) o.get(a.states + static_cast<int64_t>(w / kStateTokens) * DN, h[0]);
-            else o.get_or_zero(nullptr, 0, h[0]);
+    // The state behind a span's tokens, from the one before.
+    const auto ahead = [&](int w, float (&h)[kQuad][S]) {
+        int from = begin, to = end;
+        const Window v = window_of(bound, w, row, from, to);
+        by_span(v, [&](auto inside) {
+        constexpr bool kInside = decltype(inside)::value;
+        o.here();
+        float x[kSpan], dt[kSpan], B[kSpan][S];
 #pragma unroll
-            for (int i = 0; i < kStep; ++i) {
-                if (!(v.valid >> i & 1)) continue;
+        for (int i = 0; i < kSpan; ++i) {
+            if (!kInside && !(v.valid >> i & 1)) continue;
+            x[i] = o.template own<T>(a.s.x, a.s.x_stride, w + i);
+            dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
+            o.shared(static_cast<const T*>(a.s.b) + (w + i) * a.s.b_stride, B[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kSpan; ++i) {
+            if (!kInside && !(v.valid >> i & 1)) continue;
+            if (!kInside && (v.starts >> i & 1)) o.get_or_zero(a.s.h0, bound.at(w + i), h);
+            const float u = softplus(dt[i] + bias);
+            float us[kQuad], ins[kQuad];
+            spread(u, us);
+            spread(u * x[i], ins);
+#pragma unroll
+            for (int j = 0; j < kQuad; ++j)
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+                    h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * B[i][s]);
+        }
+        });
+    };
+    for (int w = (row.t1 - 1) / kSpan * kSpan; w + kSpan > row.t0; w -= kSpan) {
+        Window v = window_of(bound, w, row, begin, end);
+        // A sequence's tokens, the last sequence's first: a state before a sequence's first token is not the
+        // one behind the token ahead of it.
+        const auto part = [&](auto inside, uint32_t begun) {
+            constexpr bool kInside = decltype(inside)::value;
+        o.here();
+            float x[kSpan], dt[kSpan], u[kSpan], z[kSpan], dy[kSpan], B[kSpan][S], C[kSpan][S];
+            float h[kQuad][S];
+            if (!kInside && begun) {
+                o.get_or_zero(nullptr, 0, h);          // its first token takes h0
+            } else {
+                // The state that was kept, and half of the time the tokens from there to here.
+                o.get(a.states + static_cast<int64_t>(w / kStateTokens) * DN, h);
+                if (w % kStateTokens) ahead(w - kSpan, h);
+            }
+#pragma unroll
+            for (int i = 0; i < kSpan; ++i) {
+                if (!kInside && !(v.valid >> i & 1)) continue;
                 x[i] = o.template own<T>(a.s.x, a.s.x_stride, w + i);
                 dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
                 if (a.s.z) z[i] = o.template own<T>(a.s.z, a.s.z_stride, w + i);
@@ -496,35 +575,36 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const SsmBackArgs a,
                 o.shared(static_cast<const T*>(a.s.c) + (w + i) * a.s.c_stride, C[i]);
             }
 #pragma unroll
-            for (int i = 0; i < kStep; ++i) {
-                if (v.valid >> i & 1) {
-                    if (v.starts >> i & 1) o.get_or_zero(a.s.h0, bound.at(w + i), h[i]);
-                    dt[i] += bias;
-                    u[i] = o.in ? softplus(dt[i]) : 0.0f;
-                    float us[kQuad], ins[kQuad];
-                    spread(u[i], us);
-                    spread(u[i] * x[i], ins);
+            for (int i = 0; i < kSpan; ++i) {
+                if (!kInside && !(v.valid >> i & 1)) continue;
+                if (!kInside && (v.starts >> i & 1)) o.get_or_zero(a.s.h0, bound.at(w + i), h);
+                dt[i] += bias;
+                u[i] = o.in ? softplus(dt[i]) : 0.0f;
+                float us[kQuad], ins[kQuad];
+                spread(u[i], us);
+                spread(u[i] * x[i], ins);
 #pragma unroll
-                    for (int j = 0; j < kQuad; ++j)
+                for (int j = 0; j < kQuad; ++j) {
+                    States v;
 #pragma unroll
-                        for (int s = 0; s < S; ++s)
-                            h[i + 1][j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[i][j][s], ins[j] * B[i][s]);
-                } else {
+                    for (int s = 0; s < S; ++s) v[s] = h[j][s];
+                    ahead_of[i][j][lane] = v;
 #pragma unroll
-                    for (int j = 0; j < kQuad; ++j)
-#pragma unroll
-                        for (int s = 0; s < S; ++s) h[i + 1][j][s] = h[i][j][s];
+                    for (int s = 0; s < S; ++s)
+                        h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * B[i][s]);
                 }
             }
 #pragma unroll
-            for (int i = kStep - 1; i >= 0; --i) {
-                if (!(v.valid >> i & 1)) continue;
-                if (v.ends >> i & 1) o.get_or_zero(a.g.dh_last, bound.at(w + i), e);
-                float d = dy[i], g = 0.0f, rest = 0.0f;
+            for (int i = kSpan - 1; i >= 0; --i) {
+                if (!kInside && !(v.valid >> i & 1)) continue;
+                if (!kInside && (v.ends >> i & 1)) o.get_or_zero(a.g.dh_last, bound.at(w + i), e);
+                float d = o.in ? dy[i] : 0.0f, g = 0.0f, rest = 0.0f;
                 if (a.s.z) {
                     gates(z[i], g, rest);
                     d *= z[i] * g;
                 }
+                // As something new: else the decays of the way there are kept, in registers that are not there.
+                asm volatile("" : "+v"(u[i]));
                 float us[kQuad], ins[kQuad], ds[kQuad], ys[kQuad], into[kQuad], flow[kQuad], dB[S], dC[S];
                 spread(u[i], us);
                 spread(u[i] * x[i], ins);
@@ -534,35 +614,33 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const SsmBackArgs a,
 #pragma unroll
                 for (int j = 0; j < kQuad; ++j) {
                     ys[j] = into[j] = flow[j] = 0.0f;
+                    const States before = ahead_of[i][j][lane];
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
-                        const float now = h[i + 1][j][s], dh = __builtin_fmaf(C[i][s], ds[j], e[j][s]);
+                        const float now = h[j][s], dh = __builtin_fmaf(C[i][s], ds[j], e[j][s]);
                         dC[s] = __builtin_fmaf(ds[j], now, dC[s]);
                         dB[s] = __builtin_fmaf(ins[j], dh, dB[s]);
                         ys[j] = __builtin_fmaf(C[i][s], now, ys[j]);
                         into[j] = __builtin_fmaf(dh, B[i][s], into[j]);
                         e[j][s] = __builtin_amdgcn_exp2f(us[j] * A[j][s]) * dh;
-                        const float p = e[j][s] * h[i][j][s];
+                        h[j][s] = before[s];
+                        const float p = e[j][s] * before[s];
                         flow[j] = __builtin_fmaf(p, A[j][s], flow[j]);
                         dA[j][s] = __builtin_fmaf(p, us[j], dA[j][s]);
                     }
                 }
-                if (a.g.dh0 && (v.starts >> i & 1)) o.put(a.g.dh0 + bound.at(w + i) * DN, e);
+                if (!kInside && a.g.dh0 && (v.starts >> i & 1)) o.put(a.g.dh0 + bound.at(w + i) * DN, e);
                 const float in_sum = gather(into), flow_sum = gather(flow) * kLn2;
                 float keep, take;
                 gates(dt[i], keep, take);
                 const float ddt = __builtin_fmaf(x[i], in_sum, flow_sum) * keep;
-                if (o.in) {
-                    store(static_cast<T*>(a.g.dx) + (w + i) * a.g.dx_stride, o.mine, __builtin_fmaf(skip, d, u[i] * in_sum));
-                    store(static_cast<T*>(a.g.ddt) + (w + i) * a.g.ddt_stride, o.mine, ddt);
-                }
+                o.template write<T>(a.g.dx, a.g.dx_stride, w + i, __builtin_fmaf(skip, d, u[i] * in_sum));
+                o.template write<T>(a.g.ddt, a.g.ddt_stride, w + i, ddt);
                 dskip = __builtin_fmaf(d, x[i], dskip);
                 dbias += ddt;
                 if (a.s.z && a.g.dz) {
                     const float y = __builtin_fmaf(skip, x[i], gather(ys));
-                    if (o.in)
-                        store(static_cast<T*>(a.g.dz) + (w + i) * a.g.dz_stride, o.mine,
-                              dy[i] * y * __builtin_fmaf(z[i] * rest, g, g));
+                    o.template write<T>(a.g.dz, a.g.dz_stride, w + i, dy[i] * y * __builtin_fmaf(z[i] * rest, g, g));
                 }
                 // Over the sixteen lanes: from the fours next to it, twice.
 #pragma unroll
@@ -590,12 +668,21 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(const SsmBackArgs a,
             // The wave's sums of the window: [token][2][NP].
             float* shared = runs.shared + (static_cast<int64_t>(row.slice) * a.s.tokens + w) * (2 * NP);
 #pragma unroll
-            for (int k = 0; k < kStep * 2 * NP / kWave; ++k) {
+            for (int k = 0; k < kSpan * 2 * NP / kWave; ++k) {
                 const int i = (k * kWave + lane) / (2 * NP), at = (k * kWave + lane) % (2 * NP);
-                if (v.valid >> i & 1)
+                if (kInside || (v.valid >> i & 1))
                     shared[k * kWave + lane] = (mine[i][0][at] + mine[i][1][at]) + (mine[i][2][at] + mine[i][3][at]);
             }
             __builtin_amdgcn_wave_barrier();
+        };
+        if (v.valid == (1u << kSpan) - 1 && !(v.starts | v.ends)) {
+            part(std::true_type{}, 0u);
+            continue;
+        }
+        for (uint32_t left = v.valid; left; left &= ~v.valid) {
+            const uint32_t begun = left & v.starts;
+            v.valid = begun ? left & (~0u << (31 - __builtin_clz(begun))) : left;
+            part(std::false_type{}, begun);
         }
     }
     o.put(runs.params + row.run * DN, dA);
@@ -694,10 +781,10 @@ Cut cut_of(int64_t tokens, int64_t sequences, bool offsets, int64_t channels)
         if (one <= kRunLeast || one <= most || (one <= kWholeMost && sequences * slices >= kRowsLeast / 2))
             return {one * (most > one ? most / one : 1), true};
     }
-    len = over(len, kStep) * kStep;
+    len = over(len, kStateTokens) * kStateTokens;
     return {len < kRunLeast ? kRunLeast : len > kRunMost ? kRunMost : len, false};
 }
-static_assert(kRunLeast % kStep == 0 && kRunMost % kStep == 0 && kStep == kStateTokens, "runs begin where states are kept");
+static_assert(kRunLeast % kStateTokens == 0 && kRunMost % kStateTokens == 0, "runs begin where states are kept");
 
 int padded_states(int64_t state) { return state <= 8 ? 8 : 16; }
 

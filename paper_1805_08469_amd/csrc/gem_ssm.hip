@@ -83,6 +83,11 @@ template <class T> __device__ __forceinline__ T* element(T* base, uint32_t i)
 
 // ---- what a lane has --------------------------------------------------------------------
 
+// A row's values of a lane's states, at any address of their own alignment.
+template <class T, int S> struct __attribute__((packed, aligned(sizeof(T)))) Short {
+    T v[S];
+};
+
 // Its own channel `mine` (of which it computes what is one value a channel), and states [n, n + S) of the
 // four channels from `first` on.  FULL: there are 4 S states, so that a lane's are whole.
 template <int S, bool FULL> struct Lane {
@@ -157,30 +162,25 @@ template <int S, bool FULL> struct Lane {
                 for (int s = 0; s < S; ++s) h[j][s] = 0.0f;
         }
     }
-    // Its states' values of B or C (a row of N).
-    template <class T> __device__ __forceinline__ void shared(const T* row, float (&v)[S]) const
+    // Its states' values of B or C (a row of N) as they are, and as numbers.
+    template <class T> __device__ __forceinline__ Short<T, S> shared(const void* array, int64_t stride, int t) const
     {
-        if constexpr (FULL && sizeof(T) == 2 && S == 4) {
-            const Raw<T> r = *reinterpret_cast<const Raw<T>*>(element(row, n));
-            widen(r[0], r[1], v);
-        } else if constexpr (FULL && sizeof(T) == 4) {
-            using V = float __attribute__((ext_vector_type(S), aligned(4)));
-            const V r = *reinterpret_cast<const V*>(element(row, n));
+        const T* row = static_cast<const T*>(array) + t * stride;
+        if constexpr (FULL) return *reinterpret_cast<const Short<T, S>*>(element(row, n));
+        Short<T, S> r;
 #pragma unroll
-            for (int s = 0; s < S; ++s) v[s] = r[s];
-        } else {
+        for (int s = 0; s < S; ++s) r.v[s] = *element(row, static_cast<int>(n) + s < N ? n + s : N - 1);
+        return r;
+    }
+    template <class T> __device__ __forceinline__ void numbers(const Short<T, S>& r, float (&v)[S]) const
+    {
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const bool has = static_cast<int>(n) + s < N;
-                const float r = load(element(row, has ? n + s : N - 1), 0);
-                v[s] = has ? r : 0.0f;
-            }
-        }
+        for (int s = 0; s < S; ++s) v[s] = FULL || static_cast<int>(n) + s < N ? load(&r.v[s], 0) : 0.0f;
     }
     // Its channel's value; where it has none, the last channel's.
-    template <class T> __device__ __forceinline__ float own(const void* array, int64_t stride, int t) const
+    template <class T> __device__ __forceinline__ T own(const void* array, int64_t stride, int t) const
     {
-        return load(element(static_cast<const T*>(array) + t * stride, at), 0);
+        return *element(static_cast<const T*>(array) + t * stride, at);
     }
     template <class T> __device__ __forceinline__ void write(void* array, int64_t stride, int t, float v) const
     {
@@ -246,6 +246,52 @@ __device__ __forceinline__ Window window_of(const Bounds& bound, int w, const Ro
     return v;
 }
 
+// Which of a span's inputs a walk reads.
+enum : int { kX = 1, kDt = 2, kZ = 4, kB = 8, kC = 16, kDy = 32 };
+
+// A span's inputs, as they are (from load on, so that they may be on their way through the span before) and
+// as numbers.  Tokens that are not the run's have those of its first or last.
+template <class T, int S> struct Inputs {
+    T x[kSpan], dt[kSpan], z[kSpan], dy[kSpan];
+    Short<T, S> b[kSpan], c[kSpan];
+
+    template <int WHAT, class O>
+    __device__ __forceinline__ void load(O& o, const gem_ssm& s, const void* dys, int64_t dy_stride, const Row& row, int w)
+    {
+        o.here();
+        // Without a gate x stands for it, unused: a load in a branch is waited for there.
+        const void* gates_at = s.z ? s.z : s.x;
+        const int64_t gates_stride = s.z ? s.z_stride : s.x_stride;
+#pragma unroll
+        for (int i = 0; i < kSpan; ++i) {
+            int t = w + i < row.t1 ? w + i : row.t1 - 1;
+            t = t > row.t0 ? t : row.t0;
+            if constexpr (WHAT & kDt) dt[i] = o.template own<T>(s.dt, s.dt_stride, t);
+            if constexpr (WHAT & kX) x[i] = o.template own<T>(s.x, s.x_stride, t);
+            if constexpr (WHAT & kB) b[i] = o.template shared<T>(s.b, s.b_stride, t);
+            if constexpr (WHAT & kC) c[i] = o.template shared<T>(s.c, s.c_stride, t);
+            if constexpr (WHAT & kDy) dy[i] = o.template own<T>(dys, dy_stride, t);
+            if constexpr (WHAT & kZ) z[i] = o.template own<T>(gates_at, gates_stride, t);
+        }
+    }
+};
+template <int S> struct Numbers {
+    float x[kSpan], dt[kSpan], z[kSpan], dy[kSpan], B[kSpan][S], C[kSpan][S];
+
+    template <int WHAT, class T, class O> __device__ __forceinline__ void of(const O& o, const Inputs<T, S>& r)
+    {
+#pragma unroll
+        for (int i = 0; i < kSpan; ++i) {
+            if constexpr (WHAT & kX) x[i] = load(&r.x[i], 0);
+            if constexpr (WHAT & kDt) dt[i] = load(&r.dt[i], 0);
+            if constexpr (WHAT & kZ) z[i] = load(&r.z[i], 0);
+            if constexpr (WHAT & kDy) dy[i] = load(&r.dy[i], 0);
+            if constexpr (WHAT & kB) o.numbers(r.b[i], B[i]);
+            if constexpr (WHAT & kC) o.numbers(r.c[i], C[i]);
+        }
+    }
+};
+
 // f(std::true_type) for a span that is all the run's and inside a sequence, which most are: there
 // nothing stands in a branch.
 template <class F> __device__ __forceinline__ void by_span(const Window& v, F f)
@@ -275,22 +321,17 @@ __global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const Ss
     float steps = 0.0f;
     bool cut = false;          // a sequence has begun in the run
     int begin = 0, end = -1;
+    constexpr int kWhat = OUT ? kX | kDt | kZ | kB | kC : kX | kDt | kB;
+    Inputs<T, S> next;
+    next.template load<kWhat>(o, a.s, nullptr, 0, row, row.t0 / kSpan * kSpan);
     for (int w = row.t0 / kSpan * kSpan; w < row.t1; w += kSpan) {
+        Numbers<S> k;
+        k.template of<kWhat>(o, next);
+        if (w + kSpan < row.t1) next.template load<kWhat>(o, a.s, nullptr, 0, row, w + kSpan);
         const Window v = window_of(bound, w, row, begin, end);
         if (OUT && a.states && w % kStateTokens == 0 && (v.valid & 1)) o.put(a.states + static_cast<int64_t>(w / kStateTokens) * DN, h);
         by_span(v, [&](auto inside) {
         constexpr bool kInside = decltype(inside)::value;
-        o.here();
-        float x[kSpan], dt[kSpan], z[kSpan], B[kSpan][S], C[kSpan][S];
-#pragma unroll
-        for (int i = 0; i < kSpan; ++i) {
-            if (!kInside && !(v.valid >> i & 1)) continue;
-            x[i] = o.template own<T>(a.s.x, a.s.x_stride, w + i);
-            dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
-            if (OUT && a.s.z) z[i] = o.template own<T>(a.s.z, a.s.z_stride, w + i);
-            o.shared(static_cast<const T*>(a.s.b) + (w + i) * a.s.b_stride, B[i]);
-            if (OUT) o.shared(static_cast<const T*>(a.s.c) + (w + i) * a.s.c_stride, C[i]);
-        }
 #pragma unroll
         for (int i = 0; i < kSpan; ++i) {
             if (!kInside && !(v.valid >> i & 1)) continue;
@@ -299,26 +340,26 @@ __global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const Ss
                 steps = 0.0f;
                 cut = true;
             }
-            const float u = softplus(dt[i] + bias);
+            const float u = softplus(k.dt[i] + bias);
             float us[kQuad], ins[kQuad], ys[kQuad];
             spread(u, us);
-            spread(u * x[i], ins);
+            spread(u * k.x[i], ins);
             if (!OUT) steps += u;
 #pragma unroll
             for (int j = 0; j < kQuad; ++j) {
                 ys[j] = 0.0f;
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * B[i][s]);
-                    if (OUT) ys[j] = __builtin_fmaf(C[i][s], h[j][s], ys[j]);
+                    h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * k.B[i][s]);
+                    if (OUT) ys[j] = __builtin_fmaf(k.C[i][s], h[j][s], ys[j]);
                 }
             }
             if (!OUT) continue;
-            float y = __builtin_fmaf(skip, x[i], gather(ys));
+            float y = __builtin_fmaf(skip, k.x[i], gather(ys));
             if (a.s.z) {
                 float g, r;
-                gates(z[i], g, r);
-                y *= z[i] * g;
+                gates(k.z[i], g, r);
+                y *= k.z[i] * g;
             }
             o.template write<T>(a.y, a.y_stride, w + i, y);
             if (!kInside && a.h_last && (v.ends >> i & 1)) {
@@ -443,20 +484,16 @@ __global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBack
     float steps = 0.0f;
     bool cut = false;
     int begin = 0, end = -1;
+    constexpr int kWhat = kDt | kZ | kDy | kC;
+    Inputs<T, S> next;
+    next.template load<kWhat>(o, a.s, a.g.dy, a.g.dy_stride, row, (row.t1 - 1) / kSpan * kSpan);
     for (int w = (row.t1 - 1) / kSpan * kSpan; w + kSpan > row.t0; w -= kSpan) {
+        Numbers<S> k;
+        k.template of<kWhat>(o, next);
+        if (w > row.t0) next.template load<kWhat>(o, a.s, a.g.dy, a.g.dy_stride, row, w - kSpan);
         const Window v = window_of(bound, w, row, begin, end);
         by_span(v, [&](auto inside) {
         constexpr bool kInside = decltype(inside)::value;
-        o.here();
-        float dt[kSpan], z[kSpan], dy[kSpan], C[kSpan][S];
-#pragma unroll
-        for (int i = 0; i < kSpan; ++i) {
-            if (!kInside && !(v.valid >> i & 1)) continue;
-            dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
-            if (a.s.z) z[i] = o.template own<T>(a.s.z, a.s.z_stride, w + i);
-            dy[i] = o.template own<T>(a.g.dy, a.g.dy_stride, w + i);
-            o.shared(static_cast<const T*>(a.s.c) + (w + i) * a.s.c_stride, C[i]);
-        }
 #pragma unroll
         for (int i = kSpan - 1; i >= 0; --i) {
             if (!kInside && !(v.valid >> i & 1)) continue;
@@ -465,12 +502,12 @@ __global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBack
                 steps = 0.0f;
                 cut = true;
             }
-            const float u = softplus(dt[i] + bias);
-            float d = dy[i];
+            const float u = softplus(k.dt[i] + bias);
+            float d = k.dy[i];
             if (a.s.z) {
                 float g, r;
-                gates(z[i], g, r);
-                d *= z[i] * g;
+                gates(k.z[i], g, r);
+                d *= k.z[i] * g;
             }
             float us[kQuad], ds[kQuad];
             spread(u, us);
@@ -480,7 +517,7 @@ __global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBack
             for (int j = 0; j < kQuad; ++j)
 #pragma unroll
                 for (int s = 0; s < S; ++s)
-                    e[j][s] = __builtin_amdgcn_exp2f(us[j] * A[j][s]) * __builtin_fmaf(C[i][s], ds[j], e[j][s]);
+                    e[j][s] = __builtin_amdgcn_exp2f(us[j] * A[j][s]) * __builtin_fmaf(k.C[i][s], ds[j], e[j][s]);
         }
         });
     }
@@ -523,28 +560,23 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
         const Window v = window_of(bound, w, row, from, to);
         by_span(v, [&](auto inside) {
         constexpr bool kInside = decltype(inside)::value;
-        o.here();
-        float x[kSpan], dt[kSpan], B[kSpan][S];
-#pragma unroll
-        for (int i = 0; i < kSpan; ++i) {
-            if (!kInside && !(v.valid >> i & 1)) continue;
-            x[i] = o.template own<T>(a.s.x, a.s.x_stride, w + i);
-            dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
-            o.shared(static_cast<const T*>(a.s.b) + (w + i) * a.s.b_stride, B[i]);
-        }
+        Inputs<T, S> r;
+        Numbers<S> k;
+        r.template load<kX | kDt | kB>(o, a.s, nullptr, 0, row, w);
+        k.template of<kX | kDt | kB>(o, r);
 #pragma unroll
         for (int i = 0; i < kSpan; ++i) {
             if (!kInside && !(v.valid >> i & 1)) continue;
             if (!kInside && (v.starts >> i & 1)) o.get_or_zero(a.s.h0, bound.at(w + i), h);
-            const float u = softplus(dt[i] + bias);
+            const float u = softplus(k.dt[i] + bias);
             float us[kQuad], ins[kQuad];
             spread(u, us);
-            spread(u * x[i], ins);
+            spread(u * k.x[i], ins);
 #pragma unroll
             for (int j = 0; j < kQuad; ++j)
 #pragma unroll
                 for (int s = 0; s < S; ++s)
-                    h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * B[i][s]);
+                    h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * k.B[i][s]);
         }
         });
     };
@@ -554,8 +586,11 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
         // one behind the token ahead of it.
         const auto part = [&](auto inside, uint32_t begun) {
             constexpr bool kInside = decltype(inside)::value;
-        o.here();
-            float x[kSpan], dt[kSpan], u[kSpan], z[kSpan], dy[kSpan], B[kSpan][S], C[kSpan][S];
+            constexpr int kWhat = kX | kDt | kZ | kB | kC | kDy;
+            Inputs<T, S> r;
+            Numbers<S> k;
+            float u[kSpan];
+            r.template load<kWhat>(o, a.s, a.g.dy, a.g.dy_stride, row, w);
             float h[kQuad][S];
             if (!kInside && begun) {
                 o.get_or_zero(nullptr, 0, h);          // its first token takes h0
@@ -564,25 +599,16 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
                 o.get(a.states + static_cast<int64_t>(w / kStateTokens) * DN, h);
                 if (w % kStateTokens) ahead(w - kSpan, h);
             }
-#pragma unroll
-            for (int i = 0; i < kSpan; ++i) {
-                if (!kInside && !(v.valid >> i & 1)) continue;
-                x[i] = o.template own<T>(a.s.x, a.s.x_stride, w + i);
-                dt[i] = o.template own<T>(a.s.dt, a.s.dt_stride, w + i);
-                if (a.s.z) z[i] = o.template own<T>(a.s.z, a.s.z_stride, w + i);
-                dy[i] = o.template own<T>(a.g.dy, a.g.dy_stride, w + i);
-                o.shared(static_cast<const T*>(a.s.b) + (w + i) * a.s.b_stride, B[i]);
-                o.shared(static_cast<const T*>(a.s.c) + (w + i) * a.s.c_stride, C[i]);
-            }
+            k.template of<kWhat>(o, r);
 #pragma unroll
             for (int i = 0; i < kSpan; ++i) {
                 if (!kInside && !(v.valid >> i & 1)) continue;
                 if (!kInside && (v.starts >> i & 1)) o.get_or_zero(a.s.h0, bound.at(w + i), h);
-                dt[i] += bias;
-                u[i] = o.in ? softplus(dt[i]) : 0.0f;
+                k.dt[i] += bias;
+                u[i] = o.in ? softplus(k.dt[i]) : 0.0f;
                 float us[kQuad], ins[kQuad];
                 spread(u[i], us);
-                spread(u[i] * x[i], ins);
+                spread(u[i] * k.x[i], ins);
 #pragma unroll
                 for (int j = 0; j < kQuad; ++j) {
                     States v;
@@ -591,23 +617,23 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
                     ahead_of[i][j][lane] = v;
 #pragma unroll
                     for (int s = 0; s < S; ++s)
-                        h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * B[i][s]);
+                        h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * A[j][s]), h[j][s], ins[j] * k.B[i][s]);
                 }
             }
 #pragma unroll
             for (int i = kSpan - 1; i >= 0; --i) {
                 if (!kInside && !(v.valid >> i & 1)) continue;
                 if (!kInside && (v.ends >> i & 1)) o.get_or_zero(a.g.dh_last, bound.at(w + i), e);
-                float d = o.in ? dy[i] : 0.0f, g = 0.0f, rest = 0.0f;
+                float d = o.in ? k.dy[i] : 0.0f, g = 0.0f, rest = 0.0f;
                 if (a.s.z) {
-                    gates(z[i], g, rest);
-                    d *= z[i] * g;
+                    gates(k.z[i], g, rest);
+                    d *= k.z[i] * g;
                 }
                 // As something new: else the decays of the way there are kept, in registers that are not there.
                 asm volatile("" : "+v"(u[i]));
                 float us[kQuad], ins[kQuad], ds[kQuad], ys[kQuad], into[kQuad], flow[kQuad], dB[S], dC[S];
                 spread(u[i], us);
-                spread(u[i] * x[i], ins);
+                spread(u[i] * k.x[i], ins);
                 spread(d, ds);
 #pragma unroll
                 for (int s = 0; s < S; ++s) dB[s] = dC[s] = 0.0f;
@@ -617,11 +643,11 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
                     const States before = ahead_of[i][j][lane];
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
-                        const float now = h[j][s], dh = __builtin_fmaf(C[i][s], ds[j], e[j][s]);
+                        const float now = h[j][s], dh = __builtin_fmaf(k.C[i][s], ds[j], e[j][s]);
                         dC[s] = __builtin_fmaf(ds[j], now, dC[s]);
                         dB[s] = __builtin_fmaf(ins[j], dh, dB[s]);
-                        ys[j] = __builtin_fmaf(C[i][s], now, ys[j]);
-                        into[j] = __builtin_fmaf(dh, B[i][s], into[j]);
+                        ys[j] = __builtin_fmaf(k.C[i][s], now, ys[j]);
+                        into[j] = __builtin_fmaf(dh, k.B[i][s], into[j]);
                         e[j][s] = __builtin_amdgcn_exp2f(us[j] * A[j][s]) * dh;
                         h[j][s] = before[s];
                         const float p = e[j][s] * before[s];
@@ -632,15 +658,15 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
                 if (!kInside && a.g.dh0 && (v.starts >> i & 1)) o.put(a.g.dh0 + bound.at(w + i) * DN, e);
                 const float in_sum = gather(into), flow_sum = gather(flow) * kLn2;
                 float keep, take;
-                gates(dt[i], keep, take);
-                const float ddt = __builtin_fmaf(x[i], in_sum, flow_sum) * keep;
+                gates(k.dt[i], keep, take);
+                const float ddt = __builtin_fmaf(k.x[i], in_sum, flow_sum) * keep;
                 o.template write<T>(a.g.dx, a.g.dx_stride, w + i, __builtin_fmaf(skip, d, u[i] * in_sum));
                 o.template write<T>(a.g.ddt, a.g.ddt_stride, w + i, ddt);
-                dskip = __builtin_fmaf(d, x[i], dskip);
+                dskip = __builtin_fmaf(d, k.x[i], dskip);
                 dbias += ddt;
                 if (a.s.z && a.g.dz) {
-                    const float y = __builtin_fmaf(skip, x[i], gather(ys));
-                    o.template write<T>(a.g.dz, a.g.dz_stride, w + i, dy[i] * y * __builtin_fmaf(z[i] * rest, g, g));
+                    const float y = __builtin_fmaf(skip, k.x[i], gather(ys));
+                    o.template write<T>(a.g.dz, a.g.dz_stride, w + i, k.dy[i] * y * __builtin_fmaf(k.z[i] * rest, g, g));
                 }
                 // Over the sixteen lanes: from the fours next to it, twice.
 #pragma unroll

@@ -376,6 +376,50 @@ __global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const Ss
     }
 }
 
+// One token a sequence: no chain, one launch, a wave for 64 channels of a sequence.
+template <class T, int S, bool FULL>
+__global__ __launch_bounds__(kThreads) void step_kernel(const SsmArgs a, int slices)
+{
+    const int64_t rows = a.s.tokens * slices;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); i < rows;
+         i += static_cast<int64_t>(gridDim.x) * kWaves) {
+        const int t = static_cast<int>(i / slices);
+        Lane<S, FULL> o(a.s, static_cast<int>(i - static_cast<int64_t>(t) * slices));
+        const int64_t DN = static_cast<int64_t>(o.D) * o.N;
+        float A[kQuad][S], h[kQuad][S], B[S], C[S];
+        o.get_or_zero(a.s.h0, t, h);
+        o.get(a.s.a, A);
+        const T xr = o.template own<T>(a.s.x, a.s.x_stride, t), dtr = o.template own<T>(a.s.dt, a.s.dt_stride, t);
+        const T zr = a.s.z ? o.template own<T>(a.s.z, a.s.z_stride, t) : T{};
+        const Short<T, S> br = o.template shared<T>(a.s.b, a.s.b_stride, t), cr = o.template shared<T>(a.s.c, a.s.c_stride, t);
+        const float bias = o.weight(a.s.dt_bias), skip = o.weight(a.s.d);
+        if (a.states && t % kStateTokens == 0) o.put(a.states + t / kStateTokens * DN, h);
+        o.numbers(br, B);
+        o.numbers(cr, C);
+        const float x = load(&xr, 0), z = load(&zr, 0), u = softplus(load(&dtr, 0) + bias);
+        float us[kQuad], ins[kQuad], ys[kQuad];
+        spread(u, us);
+        spread(u * x, ins);
+#pragma unroll
+        for (int j = 0; j < kQuad; ++j) {
+            ys[j] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                h[j][s] = __builtin_fmaf(__builtin_amdgcn_exp2f(us[j] * (A[j][s] * kLog2e)), h[j][s], ins[j] * B[s]);
+                ys[j] = __builtin_fmaf(C[s], h[j][s], ys[j]);
+            }
+        }
+        if (a.h_last) o.put(a.h_last + t * DN, h);
+        float y = __builtin_fmaf(skip, x, gather(ys));
+        if (a.s.z) {
+            float g, r;
+            gates(z, g, r);
+            y *= z * g;
+        }
+        o.template write<T>(a.y, a.y_stride, t, y);
+    }
+}
+
 // Sequences without tokens, and ends that forward_kernel left in the place of what reached their
 // runs: those of sequences that began in an earlier one.
 __global__ __launch_bounds__(kThreads) void ends_kernel(const Runs r, const Bounds bound, int64_t DN, int64_t tokens, const float* h0,
@@ -788,11 +832,12 @@ __global__ __launch_bounds__(kThreads) void empty_kernel(const Bounds bound, boo
 
 // ---- launches ----------------------------------------------------------------------
 
-// Tokens of a run: as few as leave the launch kRowsLeast waves, two a SIMD, but no more than kRunMost
-// and no fewer than kRunLeast.  Sequences of one length that are shorter are taken whole, as many
+// Tokens of a run: as few as leave the launch kRowsLeast waves, four a SIMD, but no more than kRunMost
+// and no fewer than kRunLeast.  us, by the two: 16384 x 2048 in packed sequences forward 346 (2048, 256),
+// 320 (4096, 256), 322 (4096, 128); 32768 x 2048 both directions 2156, 2154, 2122, and 2256 (2048, 512).  Sequences of one length that are shorter are taken whole, as many
 // as that gives; longer ones are where they alone are half as many waves.
-constexpr int kRunMost = 256, kRunLeast = 16, kWholeMost = 4096;
-constexpr int64_t kRowsLeast = 2048;
+constexpr int kRunMost = 128, kRunLeast = 16, kWholeMost = 4096;
+constexpr int64_t kRowsLeast = 4096;
 
 struct Cut {
     int64_t len;
@@ -858,6 +903,12 @@ template <bool UP> void fold(const Runs& r, const gem_ssm& s, hipStream_t stream
 template <class T, int S, bool FULL> struct Launch {
     static void forward(const SsmArgs& a, const OpsDevice& d, hipStream_t stream)
     {
+        if (!a.s.offsets && a.s.tokens == a.s.sequences) {
+            const int64_t slices = over(a.s.channels, kWave);
+            hipLaunchKernelGGL((step_kernel<T, S, FULL>), loop_grid(over(a.s.tokens * slices, kWaves)), dim3(kThreads), 0, stream, a,
+                               static_cast<int>(slices));
+            return;
+        }
         Runs r = runs_of(a.s, false, d);
         const Bounds b = bounds_of(a.s);
         const int64_t DN = static_cast<int64_t>(a.s.channels) * a.s.state, n = a.s.sequences * DN;

@@ -134,8 +134,8 @@ def test_forward_and_backward(tokens, seqs, D, N, kind, dtype):
 
 @pytest.mark.gpu
 def test_longer_runs():
-    """Enough channels for runs of 24 tokens; float states through three of them."""
-    s = make(700, 5, 4096, 16, BF16, 0, "ragged")
+    """Enough channels for runs of 24 tokens."""
+    s = make(700, 5, 8192, 16, BF16, 0, "ragged")
     r = outputs(s)
     with ops_for(s) as ops:
         forward(ops, s, r)
@@ -145,7 +145,7 @@ def test_longer_runs():
 
 @pytest.mark.gpu
 def test_longest_runs():
-    """Runs of 256 tokens: two sequences, and the same tokens as four with their states handed on, which
+    """Runs of 128 tokens: two sequences, and the same tokens as four with their states handed on, which
     are cut at other places.  Decays of 0.2 a token and less forget a run's start to below a rounding,
     so outputs agree to the roundings of some ten steps (of a step: 8 of the state, N + 4 of the sum)."""
     T, D, N = 16384, 2112, 16
@@ -345,12 +345,12 @@ def test_more_elements_than_32_bits_count():
 def cut(tokens, sequences, offsets, channels):
     """Runs of a call: their number, and whether they begin with sequences."""
     slices = -(-channels // 64)
-    length = tokens * slices // 2048
+    length = tokens * slices // 4096
     if not offsets:
-        one, most = tokens // sequences, min(length, 256)
-        if one <= 16 or one <= most or (one <= 4096 and sequences * slices >= 1024):
+        one, most = tokens // sequences, min(length, 128)
+        if one <= 16 or one <= most or (one <= 4096 and sequences * slices >= 2048):
             return -(-tokens // (one * max(1, most // one))), True
-    length = min(256, max(16, -(-length // 8) * 8))
+    length = min(128, max(16, -(-length // 8) * 8))
     return -(-tokens // length), False
 
 

@@ -97,7 +97,7 @@ template <int S, bool FULL> struct Lane {
 
     // Where the lane stands, as something new: else the addresses of a loop's loads are all formed ahead of
     // it, 64 bits each, and spill.
-    __device__ __forceinline__ void here() { asm volatile("" : "+v"(at), "+v"(n)); }
+    __device__ __forceinline__ void here() { asm volatile("" : "+v"(at), "+v"(n), "+v"(first)); }
 
     __device__ Lane(const gem_ssm& s, int slice)
     {
@@ -630,6 +630,7 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
         // one behind the token ahead of it.
         const auto part = [&](auto inside, uint32_t begun) {
             constexpr bool kInside = decltype(inside)::value;
+            o.here();
             constexpr int kWhat = kX | kDt | kZ | kB | kC | kDy;
             Inputs<T, S> r;
             Numbers<S> k;

@@ -139,7 +139,7 @@ def reward(tokens: torch.Tensor, vocab: int) -> torch.Tensor:
     return (tokens[:, 1:] == (tokens[:, :-1] + 1) % vocab).float()
 
 
-def train(steps=60, workers=4, vocab=16, dim=64, sequences=32, length=16, kl=1e-4, lr=0.1, seed=0):
+def train(steps=60, workers=4, vocab=16, dim=64, sequences=32, length=16, kl=0.0, lr=0.1, seed=0):
     """Mean rewards of the answers behind each commit, and the last policy."""
     stream = torch.cuda.current_stream().cuda_stream
     g = torch.Generator(device="cuda").manual_seed(seed)

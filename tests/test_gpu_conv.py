@@ -165,6 +165,15 @@ def test_left_out():
         forward(ops, s, 20, 4, 1, last="none", before="none", bias=False)
         want = reference(s["x"], s["w"], torch.zeros_like(s["b"]), torch.zeros_like(s["before"]), s["off"], 1)
         assert off(s["y"], want["y"]) <= 0 and (s["last"] == 7).all()
+        zero = dict(s, before=torch.zeros_like(s["before"]))
+        forward(ops, s, 20, 4, 1, before="none")
+        first = s["last"].clone()
+        forward(ops, zero, 20, 4, 1)
+        assert torch.equal(first, s["last"])
+        one = make(6, 6, 20, 4, F32, 0, "equal")
+        forward(ops, one, 20, 4, 1, before="none")
+        want = reference(one["x"], one["w"], one["b"], torch.zeros_like(one["before"]), one["off"], 1)
+        assert off(one["y"], want["y"]) <= 0 and off(one["last"], want["last"]) <= 0
         e = make(0, 3, 20, 4, F32, 0, "equal")
         forward(ops, e, 20, 4, 1)
         assert torch.equal(e["last"], e["before"])

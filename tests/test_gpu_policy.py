@@ -176,6 +176,24 @@ def test_rows_out_of_the_ordinary(ops, rows, vocab):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(3, 30), (7, 20011), (300, 4099), (259, 131071)])
+def test_rows_that_start_anywhere(ops, rows, vocab, dtype):
+    """Logits and gradient of other alignments and strides, and what lies around them."""
+    z, action, old, adv, ref, w = inputs(rows, vocab, dtype)
+    want, g, g_e, _ = formula(z, 1.0, action, old, adv, ref, 0.2, 0.3, 0.1, w)
+    for a, b in ((1, 3), (3, 0), (2, 5)):
+        zs = torch.full((rows * (vocab + 3) + 8,), math.nan, device="cuda", dtype=dtype)
+        gs = torch.full((rows * (vocab + 7) + 8,), 7.0, device="cuda", dtype=dtype)
+        zv = zs[a:a + rows * (vocab + 3)].view(rows, vocab + 3)[:, :vocab]
+        gv = gs[b:b + rows * (vocab + 7)].view(rows, vocab + 7)[:, :vocab]
+        zv.copy_(z)
+        check(call(ops, zv, action, old, adv, ref, w, grad=gv), want, gv, g, g_e)
+        gv.fill_(7)
+        assert (gs == 7).all()
+
+
+@pytest.mark.gpu
 def test_gradient_is_that_of_differences(ops):
     """Central differences of the loss in its logits, away from the clip's borders: the formula's are
     those of 64 bits, the kernel's gradient stands for it."""

@@ -421,7 +421,7 @@ int gem_copy_f32(const float* src, float* dst, int64_t count, void* stream);
  * otherwise); a matrix is given by the address of its first element and the
  * elements between the starts of its rows (0: rows follow each other).
  * Addresses and strides that are multiples of 16 bytes are fastest.  Outputs
- * must not overlap inputs or each other, but for the two cases named below.
+ * must not overlap inputs or each other, but for the cases named below.
  */
 typedef struct gem_ops_handle gem_ops_t;
 
@@ -688,7 +688,7 @@ typedef struct {
 } gem_ssm;
 
 /* Scratch bytes that a gem_ops_t needs for scans of up to these sizes (the same for
- * both directions; smaller ones never need more; a call with one token a sequence
+ * both directions; smaller ones never need more; forward with one token a sequence
  * and no offsets needs none), and the rows of the states that forward keeps for
  * backward. */
 int gem_ssm_scratch(int64_t tokens, int32_t channels, int32_t state, int64_t* bytes);

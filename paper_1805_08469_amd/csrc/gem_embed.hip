@@ -102,7 +102,8 @@ template <int Q> __device__ __forceinline__ Cols piece_cols(const Pieces& p, int
 
 // ---- forward -------------------------------------------------------------------------------
 
-// ROWS places a piece, all in flight: many for the rate, one where there are few places.
+// ROWS places a piece, all in flight: many for the rate (32768 x 2048 bfloat16 of 65536 binary32 rows, tokens as
+// frequent as words, 48 us, 5.6 TB/s), one where there are few places (64 x 4096 4.9 us, the launch).
 template <class T, class TO, int ROWS, bool FEW>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(const EmbedArgs a, const Pieces p)
 {
@@ -448,6 +449,7 @@ __device__ __forceinline__ void write(TG* to, const Cols (&o)[Q], float (&v)[Q][
 // of them.  The others: all rows, or (ADD: added to what is there) those of tokens that occur, each
 // of which goes to the first of its sorted places.  kGroup rows are taken by the same lanes, and
 // the zeros of tokens that do not occur, which are most, are on their way before the first sum.
+// 32768 x 2048 bfloat16 into 65536 binary32 rows 124 us (5.0 TB/s); writing zeros alone takes 98.
 template <class T, class TG, bool FEW, bool ADD, int Q>
 __global__ __launch_bounds__(kThreads) void rows_kernel(const EmbedArgs a, const Pieces p, const Pieces ahead, int blocks_ahead, const Sums s)
 {

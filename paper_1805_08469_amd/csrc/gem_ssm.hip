@@ -93,7 +93,7 @@ template <class T, int S> struct __attribute__((packed, aligned(sizeof(T)))) Sho
 template <int S, bool FULL> struct Lane {
     int mine, first, D, N;
     uint32_t at, n;
-    bool in;
+    bool in, whole;            // whole: so has every lane of the wave
 
     // Where the lane stands, as something new: else the addresses of a loop's loads are all formed ahead of
     // it, 64 bits each, and spill.
@@ -106,6 +106,7 @@ template <int S, bool FULL> struct Lane {
         N = s.state;
         mine = slice * kWave + lane;
         in = mine < D;
+        whole = slice * kWave + kWave <= D;
         at = in ? mine : D - 1;
         first = slice * kWave + lane / kQuad * kQuad;
         n = lane % kQuad * S;
@@ -218,11 +219,12 @@ __device__ __forceinline__ bool row_of(const Runs& r, int tokens, Row& out)
     return true;
 }
 
-// kSpan tokens: bits of those that are the run's, that begin a sequence, and that end one.  begin and end are a sequence's that some token of the window before belongs to (the
-// last one scanned): where it reaches over all of this one, nothing begins or ends here.
 constexpr int kSpan = 4;                   // tokens whose inputs a lane has at a time
 static_assert(kStateTokens == 2 * kSpan, "every other span begins where a state is kept");
 
+// A span's tokens: bits of those that are the run's, that begin a sequence, and that end one.  begin and end
+// are those of a sequence that some token of the span before belongs to (the last one scanned): where it
+// reaches over all of this span, nothing begins or ends here.
 struct Window {
     uint32_t valid, starts, ends;
 };
@@ -290,6 +292,17 @@ template <int S> struct Numbers {
             if constexpr (WHAT & kC) o.numbers(r.c[i], C[i]);
         }
     }
+    // Nothing in lanes without a channel: u and all that follows are 0.
+    template <int WHAT, class O> __device__ __forceinline__ void only_own(const O& o)
+    {
+        if (o.whole) return;
+#pragma unroll
+        for (int i = 0; i < kSpan; ++i) {
+            x[i] = o.in ? x[i] : 0.0f;
+            dt[i] = o.in ? dt[i] : -kInf;
+            if constexpr (WHAT & kDy) dy[i] = o.in ? dy[i] : 0.0f;
+        }
+    }
 };
 
 // f(std::true_type) for a span that is all the run's and inside a sequence, which most are: there
@@ -302,7 +315,9 @@ template <class F> __device__ __forceinline__ void by_span(const Window& v, F f)
 
 // ---- forward ---------------------------------------------------------------------------
 
-// OUT: the outputs, from the states that reach the runs; else the runs' maps.
+// OUT: the outputs, from the states that reach the runs; else the runs' maps.  32768 x 2048 x 16 bfloat16 in
+// eight sequences: the maps 223 us, which is the time of their vector instructions (105 a token of 64
+// channels, 16 of them exponentials), the outputs with the kept states 384 (302 of vector instructions).
 template <class T, int S, bool FULL, bool OUT>
 __global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const SsmArgs a, const Runs runs, const Bounds bound)
 {
@@ -376,7 +391,8 @@ __global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const Ss
     }
 }
 
-// One token a sequence: no chain, one launch, a wave for 64 channels of a sequence.
+// One token a sequence: no chain, one launch, a wave for 64 channels of a sequence.  Bytes of the states bound
+// it: 64 x 4096 x 16 bfloat16 8.5 us (4.2 TB/s).
 template <class T, int S, bool FULL>
 __global__ __launch_bounds__(kThreads) void step_kernel(const SsmArgs a, int slices)
 {
@@ -509,6 +525,7 @@ __global__ __launch_bounds__(kFoldThreads) void fold_kernel(const Runs r, const 
 
 // ---- backward ------------------------------------------------------------------------------
 
+// The same sizes: 245 us, all of it vector instructions.
 template <class T, int S, bool FULL>
 __global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBackArgs a, const Runs runs, const Bounds bound)
 {
@@ -569,6 +586,10 @@ __global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBack
     if (o.in) runs.steps[static_cast<int64_t>(row.run) * o.D + o.mine] = cut ? -1.0f : steps;
 }
 
+// The gradients, four tokens at a time from the run's last.  The same sizes: 1210 us, 955 of them vector
+// instructions (492 a token of 64 channels).  The rest is waiting with two waves a SIMD: inputs fetched ahead as in
+// forward_kernel leave no registers, and spilled ones cost more (the step with its forward pass 4381 us
+// instead of 2073).
 template <class T, int S, bool FULL>
 __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs a, const Runs runs, const Bounds bound)
 {
@@ -598,7 +619,8 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
     const float bias = o.weight(a.s.dt_bias), skip = o.weight(a.s.d);
     float dskip = 0.0f, dbias = 0.0f;
     int begin = 0, end = -1;
-    // The state behind a span's tokens, from the one before.
+    // The state behind a span's tokens, from the one before.  (Lanes without a channel hold zeros throughout:
+    // sums over channels have them too.)
     const auto ahead = [&](int w, float (&h)[kQuad][S]) {
         int from = begin, to = end;
         const Window v = window_of(bound, w, row, from, to);
@@ -608,6 +630,7 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
         Numbers<S> k;
         r.template load<kX | kDt | kB>(o, a.s, nullptr, 0, row, w);
         k.template of<kX | kDt | kB>(o, r);
+        k.template only_own<kX | kDt>(o);
 #pragma unroll
         for (int i = 0; i < kSpan; ++i) {
             if (!kInside && !(v.valid >> i & 1)) continue;
@@ -645,12 +668,13 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
                 if (w % kStateTokens) ahead(w - kSpan, h);
             }
             k.template of<kWhat>(o, r);
+            k.template only_own<kWhat>(o);
 #pragma unroll
             for (int i = 0; i < kSpan; ++i) {
                 if (!kInside && !(v.valid >> i & 1)) continue;
                 if (!kInside && (v.starts >> i & 1)) o.get_or_zero(a.s.h0, bound.at(w + i), h);
                 k.dt[i] += bias;
-                u[i] = o.in ? softplus(k.dt[i]) : 0.0f;
+                u[i] = softplus(k.dt[i]);
                 float us[kQuad], ins[kQuad];
                 spread(u[i], us);
                 spread(u[i] * k.x[i], ins);
@@ -669,7 +693,7 @@ __global__ __launch_bounds__(kThreads, 2) void backward_kernel(const SsmBackArgs
             for (int i = kSpan - 1; i >= 0; --i) {
                 if (!kInside && !(v.valid >> i & 1)) continue;
                 if (!kInside && (v.ends >> i & 1)) o.get_or_zero(a.g.dh_last, bound.at(w + i), e);
-                float d = o.in ? k.dy[i] : 0.0f, g = 0.0f, rest = 0.0f;
+                float d = k.dy[i], g = 0.0f, rest = 0.0f;
                 if (a.s.z) {
                     gates(k.z[i], g, rest);
                     d *= k.z[i] * g;

@@ -456,17 +456,17 @@ __global__ __launch_bounds__(kThreads) void ends_kernel(const Runs r, const Boun
 
 // ---- the states between runs ---------------------------------------------------------------
 
-// Block: 32 chains (a channel's states); a thread takes kFold consecutive runs of one, 16 threads a chain,
-// so one round covers 128 runs; UP in order, else from the last.
-constexpr int kFoldChains = 32, kFoldParts = 16, kFold = 8;
-constexpr int kFoldThreads = kFoldChains * kFoldParts;
+// Block: CHAINS chains (a channel's states); a thread takes kFold consecutive runs of one, PARTS threads a chain;
+// UP in order, else from the last.  32 chains and 16 threads each go through 128 runs a round; with few channels
+// runs are many, and 16 chains and 64 threads each go through 512.
+constexpr int kFold = 8;
 
-template <bool UP>
-__global__ __launch_bounds__(kFoldThreads) void fold_kernel(const Runs r, const float* A, int D, int N)
+template <bool UP, int CHAINS, int PARTS>
+__global__ __launch_bounds__(CHAINS * PARTS) void fold_kernel(const Runs r, const float* A, int D, int N)
 {
-    __shared__ float sa[kFoldParts][kFoldChains], sb[kFoldParts][kFoldChains];
-    const int lane = threadIdx.x % kFoldChains, part = threadIdx.x / kFoldChains;
-    const int64_t DN = static_cast<int64_t>(D) * N, chain = static_cast<int64_t>(blockIdx.x) * kFoldChains + lane;
+    __shared__ float sa[PARTS][CHAINS], sb[PARTS][CHAINS];
+    const int lane = threadIdx.x % CHAINS, part = threadIdx.x / CHAINS;
+    const int64_t DN = static_cast<int64_t>(D) * N, chain = static_cast<int64_t>(blockIdx.x) * CHAINS + lane;
     const bool in = chain < DN;
     const int64_t c = in ? chain : 0;
     const float rate = A[c] * kLog2e;
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(kFoldThreads) void fold_kernel(const Runs r, const 
         b = a < 0.0f ? b : __builtin_fmaf(a, b0, b);
         a = a < 0.0f ? a : a0 < 0.0f ? a0 : a * a0;
     };
-    for (int base = 0; base < r.count; base += kFoldParts * kFold) {
+    for (int base = 0; base < r.count; base += PARTS * kFold) {
         float a[kFold], b[kFold];
 #pragma unroll
         for (int i = 0; i < kFold; ++i) {
@@ -500,7 +500,7 @@ __global__ __launch_bounds__(kFoldThreads) void fold_kernel(const Runs r, const 
             ma = na;
             mb = nb;
         }
-        for (int s = 1; s < kFoldParts; s *= 2) {              // each round doubles what a part's map covers
+        for (int s = 1; s < PARTS; s *= 2) {              // each round doubles what a part's map covers
             sa[part][lane] = ma;
             sb[part][lane] = mb;
             __syncthreads();
@@ -511,7 +511,7 @@ __global__ __launch_bounds__(kFoldThreads) void fold_kernel(const Runs r, const 
         sb[part][lane] = mb;
         __syncthreads();
         float now = part ? through(sa[part - 1][lane], sb[part - 1][lane], h) : h;
-        h = through(sa[kFoldParts - 1][lane], sb[kFoldParts - 1][lane], h);
+        h = through(sa[PARTS - 1][lane], sb[PARTS - 1][lane], h);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kFold; ++i) {
@@ -918,11 +918,18 @@ Runs runs_of(const gem_ssm& s, bool back, const OpsDevice& d)
 Bounds bounds_of(const gem_ssm& s) { return {s.offsets, s.offsets ? 0 : s.tokens / s.sequences, s.sequences}; }
 dim3 grid_of(const Runs& r) { return dim3(static_cast<unsigned>(over(static_cast<int64_t>(r.count) * r.slices, kWaves))); }
 
-template <bool UP> void fold(const Runs& r, const gem_ssm& s, hipStream_t stream)
+template <bool UP, int CHAINS, int PARTS> void fold_by(const Runs& r, const gem_ssm& s, hipStream_t stream)
 {
     const int64_t DN = static_cast<int64_t>(s.channels) * s.state;
-    hipLaunchKernelGGL((fold_kernel<UP>), dim3(static_cast<unsigned>(over(DN, kFoldChains))), dim3(kFoldThreads), 0, stream, r, s.a,
-                       s.channels, s.state);
+    hipLaunchKernelGGL((fold_kernel<UP, CHAINS, PARTS>), dim3(static_cast<unsigned>(over(DN, CHAINS))), dim3(CHAINS * PARTS), 0, stream, r,
+                       s.a, s.channels, s.state);
+}
+// Forward, us, by 32 x 16 alone and by this rule: 131072 x 64 168, 122; 65536 x 128 126, 106; 32768 x 1024 293, 299.
+constexpr int kManyRuns = 512;
+template <bool UP> void fold(const Runs& r, const gem_ssm& s, hipStream_t stream)
+{
+    if (r.count > kManyRuns) fold_by<UP, 16, 64>(r, s, stream);
+    else fold_by<UP, 32, 16>(r, s, stream);
 }
 
 template <class T, int S, bool FULL> struct Launch {

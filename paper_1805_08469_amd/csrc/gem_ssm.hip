@@ -392,7 +392,7 @@ __global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const Ss
 }
 
 // One token a sequence: no chain, one launch, a wave for 64 channels of a sequence.  Bytes of the states bound
-// it: 64 x 4096 x 16 bfloat16 8.5 us (4.2 TB/s).
+// it: 64 x 4096 x 16 bfloat16 7.5 us (4.8 TB/s); 8.5 with h0 asked for ahead of the rest.
 template <class T, int S, bool FULL>
 __global__ __launch_bounds__(kThreads) void step_kernel(const SsmArgs a, int slices)
 {
@@ -403,12 +403,12 @@ __global__ __launch_bounds__(kThreads) void step_kernel(const SsmArgs a, int sli
         Lane<S, FULL> o(a.s, static_cast<int>(i - static_cast<int64_t>(t) * slices));
         const int64_t DN = static_cast<int64_t>(o.D) * o.N;
         float A[kQuad][S], h[kQuad][S], B[S], C[S];
-        o.get_or_zero(a.s.h0, t, h);
-        o.get(a.s.a, A);
         const T xr = o.template own<T>(a.s.x, a.s.x_stride, t), dtr = o.template own<T>(a.s.dt, a.s.dt_stride, t);
         const T zr = a.s.z ? o.template own<T>(a.s.z, a.s.z_stride, t) : T{};
         const Short<T, S> br = o.template shared<T>(a.s.b, a.s.b_stride, t), cr = o.template shared<T>(a.s.c, a.s.c_stride, t);
         const float bias = o.weight(a.s.dt_bias), skip = o.weight(a.s.d);
+        o.get(a.s.a, A);
+        o.get_or_zero(a.s.h0, t, h);
         if (a.states && t % kStateTokens == 0) o.put(a.states + t / kStateTokens * DN, h);
         o.numbers(br, B);
         o.numbers(cr, C);
@@ -924,11 +924,11 @@ template <bool UP, int CHAINS, int PARTS> void fold_by(const Runs& r, const gem_
     hipLaunchKernelGGL((fold_kernel<UP, CHAINS, PARTS>), dim3(static_cast<unsigned>(over(DN, CHAINS))), dim3(CHAINS * PARTS), 0, stream, r,
                        s.a, s.channels, s.state);
 }
-// Forward, us, by 32 x 16 alone and by this rule: 131072 x 64 168, 122; 65536 x 128 126, 106; 32768 x 1024 293, 299.
-constexpr int kManyRuns = 512;
+// Few chains (less than a block a compute unit) in many runs.  Forward, us, by 32 x 16 and by 16 x 64:
+// 131072 x 64 168, 122; 65536 x 128 126, 106; 32768 x 256 107, 100; 65537 x 1001 has 23 and 30 of them.
 template <bool UP> void fold(const Runs& r, const gem_ssm& s, hipStream_t stream)
 {
-    if (r.count > kManyRuns) fold_by<UP, 16, 64>(r, s, stream);
+    if (static_cast<int64_t>(s.channels) * s.state <= 32 * 256 && r.count > 16 * kFold) fold_by<UP, 16, 64>(r, s, stream);
     else fold_by<UP, 32, 16>(r, s, stream);
 }
 

@@ -557,7 +557,7 @@ typedef struct {
  * outside [0, vocab) (padding), has outputs of 0 and its logits are not read.
  * An action whose logit is -inf has log probability -inf and ratio 0, and an
  * infinite KL term.  A row with a NaN or +inf among its logits has NaN for
- * them.  Errors: EINVAL, EDTYPE, EALIGN. */
+ * them, whatever its advantage.  Errors: EINVAL, EDTYPE, EALIGN. */
 int gem_policy_loss(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, const float* weight,
                     const gem_policy_terms* out);
 

@@ -71,8 +71,10 @@ __device__ __forceinline__ Terms terms_of(const PolicyArgs& a, const Taken& k, c
     const float lo = 1.0f - a.p.clip_low, hi = 1.0f + a.p.clip_high;
     const float held = (t.ratio < lo ? lo : t.ratio > hi ? hi : t.ratio) * adv, free = t.ratio * adv;
     const bool clipped = held < free;
-    t.loss = adv == 0.0f ? 0.0f : -(clipped ? held : free);
-    t.slope = adv == 0.0f || clipped ? 0.0f : -free;
+    // An advantage of 0 has no part, whatever the ratio, but a row without a log probability has no loss either.
+    const bool none = adv == 0.0f && t.lp == t.lp;
+    t.loss = none ? 0.0f : -(clipped ? held : free);
+    t.slope = none || clipped ? 0.0f : -free;
     t.kl = 0.0f;
     if (a.p.ref_logprob) {
         const float d = k.ref - t.lp;

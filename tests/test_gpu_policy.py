@@ -281,3 +281,22 @@ def test_refusals():
     empty = G.gem_logits(None, 0, 0, 10, G.GEM_F32, 1.0, 0)
     none = G.gem_policy(None, None, None, None, 0.2, 0.2, 0.0, 0)
     assert L.gem_policy_loss(fake, C.byref(empty), C.byref(none), None, C.byref(out)) == G.GEM_OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab", [(3, 40), (9, 20011), (300, 515), (258, 140003)])
+def test_rows_of_no_numbers_without_advantage(ops, rows, vocab):
+    """Their loss is no number, as their gradient is: an advantage of 0 leaves it out of ratios alone."""
+    for kl in (True, False):
+        for beta in (0.1, 0.0):
+            z, action, old, adv, ref, w = inputs(rows, vocab, torch.float32, seed=5)
+            action[:], w[:], adv[:] = 7, 1.0, 0.0
+            z[0, 5], z[1, 5] = math.nan, math.inf
+            dz = torch.empty_like(z)
+            for terms in (call(ops, z, action, old, adv, ref if kl else None, w, beta=beta, grad=dz),
+                          call(ops, z, action, old, adv, ref if kl else None, w, beta=beta)):
+                assert all(terms[n][:2].isnan().all() for n in TERMS if kl or n != "kl")
+                assert not any(terms[n][2:].isnan().any() for n in TERMS)
+                if not kl or beta == 0:
+                    assert (terms["loss"][2:] == 0).all()
+            assert dz[:2].isnan().all() and not dz[2:].isnan().any()

@@ -98,24 +98,24 @@ __device__ __forceinline__ void add(Run& r, const float (&x)[N], float most, flo
 }
 
 // Scores: a row's (or a part's) sums about the largest of its references; ref is 0 where
-// no logit is above -inf.
+// no logit is above -inf, t without SUM_D.
 struct Sums {
     float ref, s, t;
 };
 
-template <int WAVES>
+template <int WAVES, bool SUM_D = true>
 __device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*lds)[4])
 {
     const float top = wave_max(r.at.ref);
     float s = r.s, t = r.t;
-    if (r.at.ref > -kInf) shift_sums<true>(s, t, (r.at.ref - top) * scale - r.at.skew(scale));
+    if (r.at.ref > -kInf) shift_sums<SUM_D>(s, t, (r.at.ref - top) * scale - r.at.skew(scale));
     s = wave_sum(s);
-    t = wave_sum(t);
+    if constexpr (SUM_D) t = wave_sum(t);
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) {
         lds[wave][0] = top;
         lds[wave][1] = s;
-        lds[wave][2] = t;
+        if constexpr (SUM_D) lds[wave][2] = t;
     }
     __syncthreads();
     Sums out{lds[0][0], 0.0f, 0.0f};
@@ -124,10 +124,10 @@ __device__ __forceinline__ Sums block_sums(const Run& r, float scale, float (*ld
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
         s = lds[w][1];
-        t = lds[w][2];
-        if (lds[w][0] > -kInf) shift_sums<true>(s, t, (lds[w][0] - out.ref) * scale);
+        if constexpr (SUM_D) t = lds[w][2];
+        if (lds[w][0] > -kInf) shift_sums<SUM_D>(s, t, (lds[w][0] - out.ref) * scale);
         out.s += s;
-        out.t += t;
+        if constexpr (SUM_D) out.t += t;
     }
     if (out.ref == -kInf) out.ref = 0.0f;
     return out;

@@ -279,6 +279,7 @@ static int policy(gem_ops_t* ops, const gem_logits* z, const gem_policy* p, cons
         !aligned(grad, element(z->dtype)))
         return GEM_EALIGN;
     a.p = *p;
+    a.per_t = 1.0 / static_cast<double>(z->temperature);
     a.weight = weight;
     a.grad = grad;
     if (a.l.rows == 0) return GEM_OK;

@@ -51,6 +51,7 @@ struct DistillArgs {
 struct PolicyArgs {
     LogitArgs l;
     gem_policy p;
+    double per_t;          // 1 / temperature, for what is computed in 64 bits
     const float* weight;   // [rows] or null
     gem_policy_terms out;
     void* grad;            // rows x vocab, or null: the loss alone

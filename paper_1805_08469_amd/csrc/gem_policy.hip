@@ -37,24 +37,73 @@ template <class T> __device__ __forceinline__ Taken taken_of(const PolicyArgs& a
     return t;
 }
 
+// One value of all lanes, in a scalar register.
+__device__ __forceinline__ float of_wave(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+__device__ __forceinline__ float of_lane(float v, int lane)
+{
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+__device__ __forceinline__ Taken of_wave(const Taken& t)
+{
+    return {static_cast<int>(__builtin_amdgcn_readfirstlane(t.token)), of_wave(t.w), of_wave(t.x), of_wave(t.old), of_wave(t.ref),
+            of_wave(t.adv), t.live};
+}
+
 // Ahead of a barrier behind which the gradient may be written over the taken logit.
 __device__ __forceinline__ void is_read(float x) { asm volatile("" ::"v"(x)); }
 
-// e^d - 1 - d >= 0.  About 0, where the difference would lose what it is, from its series:
-// up to d^8 / 8!, whose next term is 2^-29 of the first at 1/4.
-__device__ __forceinline__ float kl_of(float d)
+// Ratios and the KL term are small differences of logarithms, whose 32 bits would show in them (d = 0.01 of
+// lp = -80: the KL term is off by 2^-10).  The differences are formed in 64 bits, and their exponentials and
+// series below are in 32 again, off by a few units of the result.  (The library's 64-bit functions spill 70 to
+// 89 of a lane's registers in policy_resident_kernel.)
+
+// log s, of a sum's 32 bits: its exponent's part in 64, so that the error is a unit of the mantissa's, which is
+// within sqrt(2) of 1.
+__device__ __forceinline__ double log_of(float s)
 {
-    if (__builtin_fabsf(d) < 0.25f) {
-        float s = 1.0f / 40320.0f;
-        s = __builtin_fmaf(s, d, 1.0f / 5040.0f);
-        s = __builtin_fmaf(s, d, 1.0f / 720.0f);
-        s = __builtin_fmaf(s, d, 1.0f / 120.0f);
-        s = __builtin_fmaf(s, d, 1.0f / 24.0f);
-        s = __builtin_fmaf(s, d, 1.0f / 6.0f);
-        s = __builtin_fmaf(s, d, 0.5f);
-        return s * d * d;
+    int e = __builtin_amdgcn_frexp_expf(s);
+    float m = __builtin_amdgcn_frexp_mantf(s);
+    if (m < 0.70710678f) {
+        m *= 2.0f;
+        e -= 1;
     }
-    return d > 90.0f ? kInf : expm1f(d) - d;
+    return e * 0.6931471805599453094 + static_cast<double>(__builtin_log2f(m) * kLn2);
+}
+
+// e^d: 2^k of k = d log2(e) rounded, and what rounding left of d and k by the slope.  Below 2^-126 it is 0.
+__device__ __forceinline__ float exp_of(double d)
+{
+    const float hi = static_cast<float>(d), lo = static_cast<float>(d - hi), k = hi * kLog2e;
+    constexpr float kRest = static_cast<float>(1.4426950408889634074 - kLog2e);
+    float left = __builtin_fmaf(hi, kLog2e, -k);
+    left = __builtin_fmaf(hi, kRest, left);
+    left = __builtin_fmaf(lo, kLog2e, left) * kLn2;
+    const float e = __builtin_amdgcn_exp2f(k);
+    return e == kInf || e == 0.0f ? e : __builtin_fmaf(e, left, e);
+}
+
+// kl = e^d - 1 - d >= 0 and more = e^d - 1, from d and e = e^d.  Up to |d| = 1, where the differences would lose
+// what they are, from the series of the first: up to d^11 / 11!, whose next term is 2^-27 of the sum at 1.
+__device__ __forceinline__ void kl_of(double d, float e, float& kl, float& more)
+{
+    const float hi = static_cast<float>(d);
+    if (__builtin_fabsf(hi) < 1.0f) {
+        float s = 1.0f / 39916800.0f;
+        s = __builtin_fmaf(s, hi, 1.0f / 3628800.0f);
+        s = __builtin_fmaf(s, hi, 1.0f / 362880.0f);
+        s = __builtin_fmaf(s, hi, 1.0f / 40320.0f);
+        s = __builtin_fmaf(s, hi, 1.0f / 5040.0f);
+        s = __builtin_fmaf(s, hi, 1.0f / 720.0f);
+        s = __builtin_fmaf(s, hi, 1.0f / 120.0f);
+        s = __builtin_fmaf(s, hi, 1.0f / 24.0f);
+        s = __builtin_fmaf(s, hi, 1.0f / 6.0f);
+        s = __builtin_fmaf(s, hi, 0.5f) * hi;
+        more = __builtin_fmaf(s, hi, hi);
+        kl = __builtin_fmaf(more, static_cast<float>(d - hi), s * hi);      // its slope is e^d - 1
+        return;
+    }
+    more = e - 1.0f;
+    kl = e == kInf ? e : static_cast<float>((e - 1.0) - d);
 }
 
 struct Terms {
@@ -64,11 +113,15 @@ struct Terms {
 __device__ __forceinline__ Terms terms_of(const PolicyArgs& a, const Taken& k, const Sums& u)
 {
     Terms t;
-    const float ls = __builtin_log2f(u.s);
-    t.lp = u.s != u.s ? u.s : at_most_0(log_prob(a.l, k.x, u.ref, ls));
-    t.ratio = expf(t.lp - k.old);
+    double lp = k.x == -kInf ? static_cast<double>(k.x) : (static_cast<double>(k.x) - u.ref) * a.per_t - log_of(u.s);
+    lp = u.s != u.s ? u.s : lp > 0.0 ? 0.0 : lp;       // near a single outcome its side of 0 is less than its rounding
+    t.lp = static_cast<float>(lp);
+    // Of both differences at once, lanes in turn.
+    const double gap = k.ref - lp;
+    const float grown = exp_of(threadIdx.x & 1 ? gap : lp - k.old);
+    t.ratio = of_lane(grown, 0);
     const float adv = k.adv;
-    const float lo = 1.0f - a.p.clip_low, hi = 1.0f + a.p.clip_high;
+    const float lo = of_wave(1.0f - a.p.clip_low), hi = of_wave(1.0f + a.p.clip_high);
     const float held = (t.ratio < lo ? lo : t.ratio > hi ? hi : t.ratio) * adv, free = t.ratio * adv;
     const bool clipped = held < free;
     // An advantage of 0 has no part, whatever the ratio, but a row without a log probability has no loss either.
@@ -77,11 +130,11 @@ __device__ __forceinline__ Terms terms_of(const PolicyArgs& a, const Taken& k, c
     t.slope = none || clipped ? 0.0f : -free;
     t.kl = 0.0f;
     if (a.p.ref_logprob) {
-        const float d = k.ref - t.lp;
-        t.kl = kl_of(d);
+        float more;
+        kl_of(gap, of_lane(grown, 1), t.kl, more);
         if (a.p.kl != 0.0f) {
             t.loss = __builtin_fmaf(a.p.kl, t.kl, t.loss);
-            t.slope = __builtin_fmaf(-a.p.kl, expm1f(d), t.slope);
+            t.slope = __builtin_fmaf(-a.p.kl, more, t.slope);
         }
     }
     return t;
@@ -103,9 +156,9 @@ struct Slope {
     __device__ Slope(const PolicyArgs& a, const Terms& t, const Sums& u, float w)
     {
         at.set(u.ref, a.l.scale);
-        f = w * a.l.inv_t * t.slope;
-        inv = u.s == 0.0f ? 0.0f : 1.0f / u.s;
-        c = -f * inv * __builtin_amdgcn_exp2f(-at.skew(a.l.scale));
+        f = of_wave(static_cast<float>(w * a.per_t * t.slope));
+        inv = of_wave(u.s == 0.0f ? 0.0f : 1.0f / u.s);
+        c = of_wave(-f * inv * __builtin_amdgcn_exp2f(-at.skew(a.l.scale)));
     }
     __device__ float taken(float x, float scale) const
     {
@@ -203,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(const PolicyArgs a, in
         run.at.wide = true;        // a part's sum has no skew
         run.s = p.s;
     }
-    Sums u = block_sums<WAVES>(run, scale, lds);
+    Sums u = block_sums<WAVES, false>(run, scale, lds);
     if constexpr (!(STEP & kRest)) {
         if (tid == 0) {
             // (ref, s, and ref as it is joined)
@@ -230,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(const PolicyArgs a, in
 // Loss and gradient with a row's vectors in registers, NV of a thread: what they hold is read
 // once (with REST a row has more, which is read twice).  A block goes through rows; as each
 // vector of a gradient is stored the next row's takes its place, so that loads and stores go
-// on through the sums.  4096 rows of 32768 bfloat16, an eighth without weight: 103 us (4.9 TB/s).
+// on through the sums.  4096 rows of 32768 bfloat16, an eighth without weight: 102 us (5.0 TB/s).
 constexpr int kRestUnroll = 2;
 
 template <class T, int THREADS, int NV, bool REST>
@@ -239,7 +292,7 @@ __global__ __launch_bounds__(THREADS, 4) void policy_resident_kernel(const Polic
     constexpr int WAVES = THREADS / 64, kKept = THREADS * NV;
     __shared__ float lds[2][WAVES][4];     // in turn: a wave may be a row ahead of another's last look
     const uint32_t tid = threadIdx.x;
-    const float scale = a.l.scale, reach = 20.0f / scale;
+    const float scale = a.l.scale, reach = of_wave(20.0f / scale);
     const auto part_of = [&](int64_t r) {
         return Part<T>(static_cast<const T*>(a.l.z) + r * a.l.stride, a.l.vocab, 0, a.l.vocab);
     };
@@ -282,7 +335,7 @@ __global__ __launch_bounds__(THREADS, 4) void policy_resident_kernel(const Polic
     for (int turn = 0;; turn ^= 1) {
         const Part<T> part = part_of(r);
         T* grad = grad_of(r);
-        const Taken now = taken;
+        const Taken now = of_wave(taken);
         float most = -kInf;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
@@ -328,7 +381,9 @@ __global__ __launch_bounds__(THREADS, 4) void policy_resident_kernel(const Polic
                 add<false>(run, x, most_of(x), scale, reach);
             });
         is_read(now.x);
-        const Sums sums = block_sums<WAVES>(run, scale, lds[turn]);
+        Sums sums = block_sums<WAVES, false>(run, scale, lds[turn]);
+        sums.ref = of_wave(sums.ref);
+        sums.s = of_wave(sums.s);
         const Terms m = terms_of(a, now, sums);
         if (tid == 0) write_terms(a, r, m);
         const Slope g(a, m, sums, now.w);

@@ -300,3 +300,57 @@ def test_rows_of_no_numbers_without_advantage(ops, rows, vocab):
                 if not kl or beta == 0:
                     assert (terms["loss"][2:] == 0).all()
             assert dz[:2].isnan().all() and not dz[2:].isnan().any()
+
+
+def two_tokens(rows, vocab, T, seed=0):
+    """Rows of two tokens that can occur: 0 at the last place, and the one that was taken far below it.
+    A sum of exponentials is then 1 + p, so that its logarithm is off by little (see near_formula)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = torch.full((rows, vocab), -math.inf, device="cuda")
+    z[:, -1] = 0.0
+    action = torch.randint(vocab - 1, (rows,), device="cuda", generator=g)
+    x = -3.0 - 77.0 * torch.rand(rows, device="cuda", generator=g)
+    z.scatter_(1, action[:, None], x[:, None])
+    lp = torch.log_softmax(z.double() / T, 1).gather(1, action[:, None])[:, 0]
+    old = (lp - 0.1 * torch.randn(rows, device="cuda", generator=g, dtype=torch.float64).clamp(-1.2, 1.2)).float()
+    ref = (lp + 0.02 * torch.randn(rows, device="cuda", generator=g, dtype=torch.float64)).float()
+    return z, action.to(torch.int32), old, torch.randn(rows, device="cuda", generator=g), ref
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1.0, 0.7, 3.0])
+@pytest.mark.parametrize("rows,vocab", [(3, 40), (41, 20011), (300, 515), (258, 140003)])
+def test_terms_are_differences_of_64_bits(ops, rows, vocab, T):
+    """Ratios and the KL term are differences of logarithms of up to 115 here, whose 32 bits would leave
+    errors of 64 units of 2^-24.  The sum is 1 + p: p is off by (8 |x| / T + 16) units (its exponent's
+    roundings and the exponentials'), the sum by one more rounding and a half that is its neighbour's;
+    differences are those of 64 bits, and each output has up to four roundings of its own.  The temperature is
+    the binary32 number that is passed: 0.7 itself is 1.7e-8 of it away, 2e-6 of such a logarithm."""
+    T = torch.tensor(T).item()
+    z, action, old, adv, ref = two_tokens(rows, vocab, T)
+    beta, zd = 0.5, z.double() / T
+    at = action.long()[:, None]
+    logq = torch.log_softmax(zd, 1)
+    lp = logq.gather(1, at)[:, 0]
+    p = lp.exp()
+    eps = U * (2 + p * (8 * zd.gather(1, at)[:, 0].abs() + 16))
+    ratio, gain = (lp - old.double()).exp(), adv.double()
+    ratio_e = ratio * (eps + 4 * U)
+    d = ref.double() - lp
+    kl, grown = torch.expm1(d) - d, torch.expm1(d)
+    kl_e = grown.abs() * eps + eps ** 2 + 4 * U * kl
+    free, held = ratio * gain, ratio.clamp(0.8, 1.3) * gain
+    loss = beta * kl - torch.minimum(free, held)
+    loss_e = gain.abs() * ratio_e + beta * kl_e + 4 * U * loss.abs()
+    slope = torch.where(free <= held, -free, 0.0) - beta * grown
+    slope_e = gain.abs() * ratio_e + beta * (d.exp() * eps + 4 * U * grown.abs()) + 4 * U * slope.abs()
+    dz = torch.empty_like(z)
+    for terms in (call(ops, z, action, old, adv, ref, None, T, beta=beta),
+                  call(ops, z, action, old, adv, ref, None, T, beta=beta, grad=dz)):
+        for n, v, e in (("logprob", lp, eps + U * lp.abs()), ("ratio", ratio, ratio_e), ("kl", kl, kl_e), ("loss", loss, loss_e)):
+            off = ((terms[n].double() - v).abs() - e).max().item()
+            assert off <= 0, (n, off)
+    got = dz.gather(1, at)[:, 0].double()
+    want = slope / T * (1 - p)
+    off = ((got - want).abs() - slope_e / T - want.abs() * 4 * U - (slope / T).abs() * p * U * (8 * zd.gather(1, at)[:, 0].abs() + 16)).max().item()
+    assert off <= 0, off

@@ -292,7 +292,7 @@ template <int S> struct Numbers {
             if constexpr (WHAT & kC) o.numbers(r.c[i], C[i]);
         }
     }
-    // Nothing in lanes without a channel: u and all that follows are 0.
+    // Nothing in lanes without a channel, whatever the last channel holds: u, the gate and all that follows are 0.
     template <int WHAT, class O> __device__ __forceinline__ void only_own(const O& o)
     {
         if (o.whole) return;
@@ -301,6 +301,7 @@ template <int S> struct Numbers {
             x[i] = o.in ? x[i] : 0.0f;
             dt[i] = o.in ? dt[i] : -kInf;
             if constexpr (WHAT & kDy) dy[i] = o.in ? dy[i] : 0.0f;
+            if constexpr (WHAT & kZ) z[i] = o.in ? z[i] : 0.0f;
         }
     }
 };

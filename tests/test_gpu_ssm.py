@@ -420,3 +420,28 @@ def test_refusals():
     for bad in ((-1, 1, 1), (2 ** 31 - 1, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 17), (1, 2 ** 27, 2)):
         assert L.gem_ssm_scratch(*bad, C.byref(n)) == G.GEM_EINVAL
     assert L.gem_ssm_scratch(1, 1, 1, None) == L.gem_ssm_state_rows(-1, C.byref(n)) == G.GEM_EINVAL
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,N", [(1, 16), (65, 16), (67, 5), (190, 8)])
+def test_an_infinite_gate_of_the_last_channel(D, N, dtype):
+    """Lanes beside it have no channel and add nothing: sums over channels are infinite, of the last
+    channel's sign, where its gradient is, and what they were in the other sequence."""
+    s = make(40, 2, D, N, dtype)
+    t = 9
+    for n in ("x", "c", "dy"):             # none that bfloat16 or a product makes 0
+        s[n][:] = torch.where(s[n].abs() < 0.25, 0.25, s[n])
+    r, first = outputs(s), outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, first)
+        backward(ops, s, first)
+        s["z"][t, -1] = float("inf")
+        forward(ops, s, r)
+        backward(ops, s, r)
+    sign = (s["dy"][t, -1] * s["c"][t]).sign()
+    assert r["db"][:t + 1].isinf().all()
+    assert torch.equal(r["db"][:t + 1].sign(), s["x"][:t + 1, -1:].sign() * sign)
+    assert r["dc"][t].isinf().all()
+    assert torch.equal(r["db"][t + 1:], first["db"][t + 1:]) and torch.equal(r["dc"][t + 1:], first["dc"][t + 1:])
+    assert torch.equal(r["dc"][:t], first["dc"][:t])

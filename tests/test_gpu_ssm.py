@@ -445,3 +445,122 @@ def test_an_infinite_gate_of_the_last_channel(D, N, dtype):
     assert r["dc"][t].isinf().all()
     assert torch.equal(r["db"][t + 1:], first["db"][t + 1:]) and torch.equal(r["dc"][t + 1:], first["dc"][t + 1:])
     assert torch.equal(r["dc"][:t], first["dc"][:t])
+
+
+def slow(s):
+    """Steps of about 0.004 and rates of 0.25 to 4: states live for a thousand tokens, so that what a round or a
+    run hands on stands in all outputs behind it."""
+    s["dt_bias"] -= s["dt_bias"] + 6
+    s["a"] *= 0.25
+    return s
+
+
+def lengths(s, off):
+    """Other sequences of the same tokens."""
+    seqs = len(off) - 1
+    g = torch.Generator().manual_seed(seqs)
+    D, N = s["a"].shape
+    s.update({n: torch.randn(seqs, D, N, generator=g).cuda() for n in ("h0", "dh_last")})
+    s.update(off=off, offsets=torch.tensor(off, device="cuda"))
+    return s
+
+
+def of_channels(s, r, pick):
+    """Inputs and outputs of some channels.  The others have x = dy = 0 and add exact zeros to what channels share."""
+    rows, channels, states = ("x", "dt", "z", "dy", "y", "dx", "ddt", "dz"), ("d", "dt_bias", "a", "dd", "ddt_bias", "da"), \
+        ("h0", "dh_last", "h_last", "dh0")
+
+    def part(n, t):
+        if t is None or n in ("off", "offsets", "b", "c", "db", "dc", "states"):
+            return t
+        return t[:, pick] if n in rows + states else t[pick]
+    return {n: part(n, t) for n, t in s.items()}, {n: part(n, t) for n, t in r.items()}
+
+
+def only(s, pick):
+    for n in ("x", "dy"):
+        keep = s[n][:, pick].clone()
+        s[n][:] = 0
+        s[n][:, pick] = keep
+    return s
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tokens,D,off,runs", [(9001, 60, None, 563), (8711, 64, [0, 37, 37, 8200, 8711], 545), (2203, 560, None, 138),
+                                               (2170, 531, [0, 2050, 2053, 2170], 136)])
+def test_states_handed_on_over_rounds(tokens, D, off, runs, dtype):
+    """More runs than one round of the composition takes: 512 with few states, else 128; both directions."""
+    s = slow(make(tokens, 1, D, 16, dtype))
+    if off:
+        lengths(s, off)
+    assert cut(tokens, len(s["off"]) - 1, bool(off), D) == (runs, False)
+    assert runs > (512 if 16 * D <= 8192 else 128)
+    r = outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, r)
+        backward(ops, s, r)
+        h = s["h0"].clone()                # kept in place
+        again = dict(r, y=torch.empty_like(r["y"]), h_last=h)
+        forward(ops, dict(s, h0=h), again)
+    check(r, wanted(s))
+    assert torch.equal(h, r["h_last"]) and torch.equal(again["y"], r["y"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,off,gated", [(F32, [0, 5003, 5003, 5004, 12347, 16501], True), (BF16, None, False)])
+def test_longest_runs_in_both_directions(dtype, off, gated):
+    """Runs of 128 tokens, sequences that begin and end inside of them."""
+    tokens, D = 16501, 2112
+    s = slow(make(tokens, 1, D, 16, dtype, 0, "equal", gated))
+    if off:
+        lengths(s, off)
+    assert cut(tokens, len(s["off"]) - 1, bool(off), D) == (129, False)
+    pick = torch.tensor([0, 1, 2, 3, 5, 63, 64, 100, 127, 128, 1000, 1001, 2047, 2048, 2110, 2111], device="cuda")
+    only(s, pick)
+    r = outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, r)
+        backward(ops, s, r)
+    some, got = of_channels(s, r, pick)
+    check(got, wanted(some))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [16, 8, 11])
+@pytest.mark.parametrize("seqs,each,length", [(128, 20, 40), (121, 21, 21), (32, 50, 50), (32, 333, 333), (97, 43, 43)])
+def test_sequences_taken_whole(seqs, each, length, N, dtype):
+    """Several sequences of more than 16 tokens in a run, and long ones where they alone are enough rows; runs
+    that begin at tokens of any number."""
+    tokens, D = seqs * each, 4100
+    assert cut(tokens, seqs, False, D) == (tokens // length, True)
+    s = slow(make(tokens, seqs, D, N, dtype))
+    pick = torch.tensor([0, 1, 62, 63, 64, 65, 130, 4030, 4031, 4032, 4095, 4096, 4099], device="cuda")
+    only(s, pick)
+    r = outputs(s)
+    with ops_for(s) as ops:
+        forward(ops, s, r)
+        backward(ops, s, r)
+        h = s["h0"].clone()
+        again = dict(r, y=torch.empty_like(r["y"]), h_last=h)
+        forward(ops, dict(s, h0=h), again)
+    some, got = of_channels(s, r, pick)
+    check(got, wanted(some))
+    assert torch.equal(h, r["h_last"]) and torch.equal(again["y"], r["y"])
+
+
+@pytest.mark.gpu
+def test_offsets_of_any_values_keep_states_in_place_inside():
+    """States kept in place between values that are watched."""
+    n, seqs = 60, 5
+    for bad in ([0, 70, 10, -5, 900, 60], [5, 4, 3, 2, 1, 0], [0] * 6, [60] * 6, [-2 ** 62, 2 ** 62, 3, 3, 40, 2 ** 40], [10, 20, 30, 40, 50, 55]):
+        s = make(n, seqs, 33, 16, F32, 0, "ragged")
+        s["offsets"] = torch.tensor(bad, device="cuda")
+        m = s["h0"].numel()
+        room = torch.full((3 * m,), 7.0, device="cuda")
+        h = room[m:2 * m].view(s["h0"].shape).copy_(s["h0"])
+        with ops_for(s) as ops:
+            forward(ops, dict(s, h0=h), dict(outputs(s), h_last=h))
+        torch.cuda.synchronize()
+        assert (room[:m] == 7).all() and (room[2 * m:] == 7).all(), bad

@@ -317,3 +317,50 @@ def test_refusals():
     for k in ("dy", "dlast", "dx", "dw", "db", "dbefore"):
         assert backward(**{k: 66}) == G.GEM_EALIGN, k
     assert L.gem_conv_scratch(-1, 1, C.byref(n)) == L.gem_conv_scratch(1, 0, C.byref(n)) == L.gem_conv_scratch(1, 1, None) == G.GEM_EINVAL
+
+
+def run_length(tokens, D, dtype, backward):
+    """Tokens of a call's runs: the most, halved down to 16 until they leave enough rows of 256 bytes."""
+    slices = -(-D * dtype.itemsize // 256)
+    length, least = (128, 4096) if backward else (64, 8192)
+    while length > 16 and -(-tokens // length) * slices < least:
+        length //= 2
+    return length
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tokens,D,seqs,kind,ahead,behind", [
+    (17001, 4099, 21, "ragged", 64, 128), (17010, 4100, 5, "equal", 64, 128), (5003, 4100, 9, "ragged", 32, 64), (2502, 4098, 3, "equal", 16, 32)])
+def test_longer_runs(tokens, D, seqs, kind, ahead, behind, dtype):
+    """Runs of up to 64 tokens forward and 128 backward, sequences that begin and end inside of them."""
+    if dtype == BF16:                      # twice as many channels a row
+        D = 2 * D - 1
+    assert (run_length(tokens, D, dtype, False), run_length(tokens, D, dtype, True)) == (ahead, behind)
+    W = 4
+    s = make(tokens, seqs, D, W, dtype, 3 if kind == "ragged" else 0, kind)
+    pick = torch.tensor([0, 1, 2, 3, 4, 63, 64, 127, 128, 129, 1000, 2047, D - 130, D - 129, D - 66, D - 5, D - 2, D - 1], device="cuda")
+    with ops_for(tokens, D) as ops:
+        forward(ops, s, D, W, 1)
+        backward(ops, s, D, W, 1)
+    want = reference(s["x"][:, pick], s["w"][pick], s["b"][pick], s["before"][:, :, pick], s["off"], 1, s["dy"][:, pick], s["dlast"][:, :, pick])
+    for n, got in dict(y=s["y"][:, pick], last=s["last"][:, :, pick], dx=s["dx"][:, pick], dweight=s["dw"][pick], dbias=s["db"][pick],
+                       dbefore=s["dbefore"][:, :, pick]).items():
+        assert off(got, want[n]) <= 0, (n, off(got, want[n]))
+    assert (s["y"][:, D:] == 7).all() and (s["dx"][:, D:] == 7).all()
+
+
+@pytest.mark.gpu
+def test_offsets_of_any_values_keep_inputs_in_place_inside():
+    """Inputs kept in place between values that are watched."""
+    n, seqs, D, W = 60, 5, 33, 4
+    for bad in ([0, 70, 10, -5, 900, 60], [5, 4, 3, 2, 1, 0], [0] * 6, [60] * 6, [-2 ** 62, 2 ** 62, 3, 3, 40, 2 ** 40], [10, 20, 30, 40, 50, 55]):
+        s = make(n, seqs, D, W, F32, 0, "ragged")
+        s["offsets"] = torch.tensor(bad, device="cuda")
+        m = s["before"].numel()
+        room = torch.full((3 * m,), 7.0, device="cuda")
+        s["before"] = room[m:2 * m].view(s["before"].shape).copy_(s["before"])
+        with ops_for(n, D) as ops:
+            forward(ops, s, D, W, 1, last="before")
+        torch.cuda.synchronize()
+        assert (room[:m] == 7).all() and (room[2 * m:] == 7).all(), bad

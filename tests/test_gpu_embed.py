@@ -248,3 +248,44 @@ def test_scratch_too_small():
         with pytest.raises(G.GemError) as err:
             backward(ops, tok, 10, x[:4], x)
         assert err.value.code == G.GEM_ESCRATCH
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count,vocab,dim,rows", [(1300003, 3001, 5, F32), (2200001, 70001, 3, BF16)])
+def test_more_places_than_tiles_of_one_share(count, vocab, dim, rows):
+    """Past 2^20 places a block of the sort goes through its tile several times."""
+    for kind in ("words", "even"):
+        g = torch.Generator(device="cuda").manual_seed(count)
+        tok = tokens_of(kind, count, vocab, g)
+        dout = torch.randn(count, dim, device="cuda", generator=g).to(rows)
+        grad, again = torch.full((vocab, dim), 7.0, device="cuda"), torch.full((vocab, dim), 7.0, device="cuda")
+        with ops_for(count, vocab, dim) as ops:
+            backward(ops, tok, vocab, dout, grad, 0.3)
+            backward(ops, tok, vocab, dout, again, 0.3)
+        total, err, there = want_of(tok, vocab, dout, 0.3)
+        check(grad, total, err)
+        assert (grad[~there] == 0).all() and torch.equal(grad, again)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,master", [(F32, F32), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("count,vocab,dim", [(20011, 3001, 515), (16384, 40, 1027), (33333, 9001, 260)])
+def test_chunks_of_chunks_in_wide_rows(count, vocab, dim, rows, master):
+    """Rows of more columns than a piece of lanes has, of tokens with chunks of chunks."""
+    for kind, pad in (("words", 0), ("one", 3)):
+        g = torch.Generator(device="cuda").manual_seed(count + pad)
+        tok = tokens_of(kind, count, vocab, g)
+        dout = wide(count, dim, pad, rows)[:, :dim]
+        dout.copy_(torch.randn(count, dim, device="cuda", generator=g))
+        grad = wide(vocab, dim, pad, master, 7.0)
+        base = torch.randn(vocab, dim + pad, device="cuda", generator=g).to(master)
+        added = base.clone()
+        with ops_for(count, vocab, dim) as ops:
+            backward(ops, tok, vocab, dout, grad[:, :dim], 0.3)
+            backward(ops, tok, vocab, dout, added[:, :dim], 0.3, add=1)
+        total, err, there = want_of(tok, vocab, dout, 0.3)
+        check(grad[:, :dim], total, err)
+        assert (grad[:, :dim][~there] == 0).all() and (grad[:, dim:] == 7).all()
+        both = total + base[:, :dim].double()
+        check(added[:, :dim], both, err + U * both.abs())
+        assert torch.equal(added[:, :dim][~there], base[:, :dim][~there]) and torch.equal(added[:, dim:], base[:, dim:])

@@ -925,11 +925,12 @@ template <bool UP, int CHAINS, int PARTS> void fold_by(const Runs& r, const gem_
     hipLaunchKernelGGL((fold_kernel<UP, CHAINS, PARTS>), dim3(static_cast<unsigned>(over(DN, CHAINS))), dim3(CHAINS * PARTS), 0, stream, r,
                        s.a, s.channels, s.state);
 }
-// Few chains (less than a block a compute unit) in many runs.  Forward, us, by 32 x 16 and by 16 x 64:
-// 131072 x 64 168, 122; 65536 x 128 126, 106; 32768 x 256 107, 100; 65537 x 1001 has 23 and 30 of them.
-template <bool UP> void fold(const Runs& r, const gem_ssm& s, hipStream_t stream)
+// Few chains (blocks of 32 are no more than one a compute unit) in many runs.  A forward call, us, with 32 x 16 and
+// with 16 x 64: 131072 tokens of 64 channels 168, 122; 65536 of 128 126, 106; 32768 of 256 107, 100.  Where chains
+// are more, 64 threads each are too many: the composition alone of 65537 of 1001 23, 30.
+template <bool UP> void fold(const Runs& r, const gem_ssm& s, const OpsDevice& d, hipStream_t stream)
 {
-    if (static_cast<int64_t>(s.channels) * s.state <= 32 * 256 && r.count > 16 * kFold) fold_by<UP, 16, 64>(r, s, stream);
+    if (static_cast<int64_t>(s.channels) * s.state <= int64_t{32} * d.cus && r.count > 16 * kFold) fold_by<UP, 16, 64>(r, s, stream);
     else fold_by<UP, 32, 16>(r, s, stream);
 }
 
@@ -947,7 +948,7 @@ template <class T, int S, bool FULL> struct Launch {
         const int64_t DN = static_cast<int64_t>(a.s.channels) * a.s.state, n = a.s.sequences * DN;
         if (!r.whole) {
             hipLaunchKernelGGL((forward_kernel<T, S, FULL, false>), grid_of(r), dim3(kThreads), 0, stream, a, r, b);
-            fold<true>(r, a.s, stream);
+            fold<true>(r, a.s, d, stream);
         }
         r.in_place = !r.whole && a.h_last && a.h_last == a.s.h0;
         hipLaunchKernelGGL((forward_kernel<T, S, FULL, true>), grid_of(r), dim3(kThreads), 0, stream, a, r, b);
@@ -962,7 +963,7 @@ template <class T, int S, bool FULL> struct Launch {
         const int64_t DN = static_cast<int64_t>(a.s.channels) * a.s.state, n = a.s.sequences * DN;
         if (!r.whole) {
             hipLaunchKernelGGL((backward_map_kernel<T, S, FULL>), grid_of(r), dim3(kThreads), 0, stream, a, r, b);
-            fold<false>(r, a.s, stream);
+            fold<false>(r, a.s, d, stream);
         }
         hipLaunchKernelGGL((backward_kernel<T, S, FULL>), grid_of(r), dim3(kThreads), 0, stream, a, r, b);
         constexpr int NP = kQuad * S;

@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void before_kernel(const ConvBackArgs a, 
 
 // ---- backward ------------------------------------------------------------------------------
 
-// The same sizes: 107 us, 4.0 TB/s; its vector instructions, some 45 an element, take two thirds of that.
+// The same sizes: 106 us, 4.0 TB/s; its vector instructions, 39 an element, take 73 of that.
 // Tokens of a step: with eight the registers leave two waves a SIMD (32768 x 2048 bfloat16, both
 // directions, 173 us; 164 with four).
 constexpr int kBack = 4;
@@ -441,7 +441,9 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(const ConvBackArgs a, con
 
 // ---- launches ----------------------------------------------------------------------
 
-// Tokens of a run: the most that leave the launch `least` rows of 32 lanes.
+// Tokens of a run: the most that leave the launch `least` rows of 32 lanes.  us backward, with half of kBackwardRows,
+// these and twice as many: 8192 x 2048 bfloat16 48, 40, 53; 16384 x 2048 77, 56, 73; 32768 x 512 52, 47, 70.  Forward
+// they are within 3% (16384 x 2048 28.3, 28.7, 29.6).
 constexpr int kForwardMost = 64, kBackwardMost = 128, kRunLeast = 16;
 constexpr int64_t kForwardRows = 8192, kBackwardRows = 4096;
 int run_len(int64_t tokens, int64_t slices, int most, int64_t least)

@@ -149,7 +149,9 @@ __device__ __forceinline__ void clear(Segment* seg, int vocab)
 }
 
 // Few places: each one's rank, by comparing it with all.  A block has 64 of them, a lane each, and
-// its sixteen waves a sixteenth of all to compare with.  8192 places: 64 M comparisons.
+// its sixteen waves a sixteenth of all to compare with.  2047 places take 8 us and 8192, 64 M comparisons, 19.
+// The gradient of n x 64 bfloat16 into 50021 rows, us, ranked and sorted: 4096 22, 29; 8192 30, 31; 12288 38, 34.
+// (The blocks clear the segments too, 18 of the 20 us that one block takes for 64 places of 160000 tokens.)
 constexpr int kRankMost = 8192, kRankThreads = 1024;
 
 __global__ __launch_bounds__(kRankThreads) void rank_kernel(const int32_t* tokens, int n, int vocab, int32_t* keys, int32_t* places,
@@ -582,7 +584,8 @@ struct Layout {
     }
 };
 
-// From this many places on chunks of chunks are worth a launch.
+// From this many places on chunks of chunks are worth a launch: n x 1024 bfloat16 into 32768 rows, tokens as frequent as
+// words, us, with them and without: 8192 56, 53; 16384 64, 60; 32768 64, 65; 131072 124, 136.
 constexpr int kBigLeast = 1 << 14;
 
 template <class T, class TO, bool FEW> hipError_t forward(const EmbedArgs& a, hipStream_t stream)

@@ -317,8 +317,8 @@ template <class F> __device__ __forceinline__ void by_span(const Window& v, F f)
 // ---- forward ---------------------------------------------------------------------------
 
 // OUT: the outputs, from the states that reach the runs; else the runs' maps.  32768 x 2048 x 16 bfloat16 in
-// eight sequences: the maps 223 us, which is the time of their vector instructions (105 a token of 64
-// channels, 16 of them exponentials), the outputs with the kept states 384 (302 of vector instructions).
+// eight sequences: the maps 224 us, which is the time of their vector instructions (105 a token of 64
+// channels, 16 of them exponentials), the outputs with the kept states 384 (305 of vector instructions).
 template <class T, int S, bool FULL, bool OUT>
 __global__ __launch_bounds__(kThreads, OUT ? 3 : 4) void forward_kernel(const SsmArgs a, const Runs runs, const Bounds bound)
 {
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(CHAINS * PARTS) void fold_kernel(const Runs r, cons
 
 // ---- backward ------------------------------------------------------------------------------
 
-// The same sizes: 245 us, all of it vector instructions.
+// The same sizes: 243 us, all of it vector instructions.
 template <class T, int S, bool FULL>
 __global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBackArgs a, const Runs runs, const Bounds bound)
 {
@@ -587,8 +587,8 @@ __global__ __launch_bounds__(kThreads, 4) void backward_map_kernel(const SsmBack
     if (o.in) runs.steps[static_cast<int64_t>(row.run) * o.D + o.mine] = cut ? -1.0f : steps;
 }
 
-// The gradients, four tokens at a time from the run's last.  The same sizes: 1210 us, 955 of them vector
-// instructions (492 a token of 64 channels).  The rest is waiting with two waves a SIMD: inputs fetched ahead as in
+// The gradients, four tokens at a time from the run's last.  The same sizes: 1190 us, 921 of them vector
+// instructions (473 a token of 64 channels).  The rest is waiting with two waves a SIMD: inputs fetched ahead as in
 // forward_kernel leave no registers, and spilled ones cost more (the step with its forward pass 4381 us
 // instead of 2073).
 template <class T, int S, bool FULL>
@@ -858,10 +858,14 @@ __global__ __launch_bounds__(kThreads) void empty_kernel(const Bounds bound, boo
 
 // ---- launches ----------------------------------------------------------------------
 
-// Tokens of a run: as few as leave the launch kRowsLeast waves, four a SIMD, but no more than kRunMost
-// and no fewer than kRunLeast.  us, by the two: 16384 x 2048 in packed sequences forward 346 (2048, 256),
-// 320 (4096, 256), 322 (4096, 128); 32768 x 2048 both directions 2156, 2154, 2122, and 2256 (2048, 512).  Sequences of one length that are shorter are taken whole, as many
-// as that gives; longer ones are where they alone are half as many waves.
+// Tokens of a run: the most that leave the launch kRowsLeast waves, four a SIMD, rounded up to where states are kept,
+// but no more than kRunMost and no fewer than kRunLeast.  us, by (kRowsLeast, kRunMost): 16384 x 2048 in packed
+// sequences forward 346 (2048, 256), 320 (4096, 256), 322 (4096, 128); 32768 x 2048 both directions 2156, 2154, 2122,
+// and 2256 (2048, 512).
+// Sequences of one length that are shorter are taken whole, as many as that gives; longer ones are where they alone are
+// half as many waves.  us forward and in both directions, whole and cut: 64 x 512 tokens x 2048 channels (2048 waves)
+// 394, 1681 and 564, 2068; 128 x 256 x 1024 (2048) 196, 853 and 301, 1093; but 32 x 512 x 2048 (1024 waves) 254, 1163
+// and 301, 1087.  Past kWholeMost they are cut, which costs forward a third: 64 x 8192 x 2048 6162, 26386 and 8397, 31243.
 constexpr int kRunMost = 128, kRunLeast = 16, kWholeMost = 4096;
 constexpr int64_t kRowsLeast = 4096;
 
@@ -975,7 +979,8 @@ template <class T, int S, bool FULL> struct Launch {
     }
 };
 
-// f(Launch<T, S, FULL>) for the states at hand.
+// f(Launch<T, S, FULL>) for the states at hand: whole vectors of them for the most, 16, and else each by itself, which
+// costs (64 x 4096 single tokens of 16 states 7 us, of 8 14; 32768 x 2048 both directions 2058 and 1594).
 template <class T, class F> void by_states(int state, F f)
 {
     if (state == 16) f(Launch<T, 4, true>{});

@@ -15,7 +15,7 @@ def scan(s, off, backward=True):
 
     Each bound follows its value: a product or a sum adds the roundings of what it handles, an exponential
     four and four times its exponent's size, a sigmoid 8 + 2 |v|.  A sum over N states has N + 4, over D
-    channels D / 4 + 24 (four in a lane, then steps that double), over tokens 300 + T / 64 (a run's 256,
+    channels D / 4 + 24 (four in a lane, then steps that double), over tokens 300 + T / 64 (a run's 128,
     then the runs' by fours).  All are doubled for terms of the second order and states that several
     runs' products reach."""
     s = {k: np.asarray(v, np.float64) if v is not None else None for k, v in s.items()}
